@@ -493,7 +493,7 @@ def sources_sha16():
     """Fingerprint of the sources that decide the attention launch's memory traffic (kernels and planner)."""
     import hashlib
     h = hashlib.sha256()
-    for f in ("kernels.hip", "plan.cpp"):
+    for f in ("kernels.hip", "steps.h", "plan.cpp"):
         h.update(open(os.path.join(ROOT, "paper_2602_14516_amd", "csrc", f), "rb").read())
     return h.hexdigest()[:16]
 

@@ -7,7 +7,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libampd.so")
 SOURCES = ["kernels.hip", "api.cpp", "api_host.cpp", "plan.cpp"]
-HEADERS = ["kernels.h", "plan.h", "api_host.h", os.path.join(INCLUDE, "ampd.h")]
+HEADERS = ["kernels.h", "steps.h", "plan.h", "api_host.h", os.path.join(INCLUDE, "ampd.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 
