@@ -226,6 +226,95 @@ ampd_status ampd_paged_attn(const ampd_kv_cache *cache, const ampd_batch *batch,
                             const void *q, void *out, void *workspace, size_t workspace_bytes,
                             void *stream, const ampd_plan_options *opts);
 
+/* ---- sparse attention over a long cache -----------------------------------------------------
+ *
+ * A serving step that attends a chosen part of a long history:
+ *   ampd_rope_kv_append   rotate Q and K by their positions, write K and V into the pages, keep the pages' bounds up to date;
+ *   ampd_select_pages     score every page from its bounds, choose `budget` pages for every group of queries and KV head;
+ *   ampd_sparse_attn      attention of the group's queries over the chosen pages.
+ * ampd_page_bounds_update brings the bounds of pages up to date that were written another way (ampd_kv_append,
+ * ampd_kv_unpack, an attention call that appends).
+ * All of them take their lengths as kernel arguments, enqueue kernels only and touch no staging buffer, so they may be
+ * recorded into a graph; a replay repeats the call with the lengths it was recorded with.  Physical page ids of the block
+ * table outside [0, num_pages) are skipped: such a page is neither written nor attended. */
+
+/* Position rotation: element pair (x1, x2) of a head at position t becomes
+ * scale * (x1 cos a - x2 sin a, x2 cos a + x1 sin a), a = t * inv_freq[j] (the product and its cosine and sine in 64 bits).
+ * Pair j is elements (j, j + rotary_dim/2), or (2j, 2j+1) when interleaved; elements from rotary_dim on stay as they are. */
+typedef struct {
+    int32_t rotary_dim;         /* a multiple of 16, 16 .. head_dim */
+    int32_t interleaved;        /* 0 or 1 */
+    const float *inv_freq;      /* DEVICE [rotary_dim / 2], radians per position */
+    const int32_t *positions;   /* DEVICE [sum L]: position of each packed token; NULL: token i of request r is at C_r + i */
+    float scale;                /* finite, > 0; 1 for the plain rotation */
+    int32_t reserved;           /* must be 0 */
+} ampd_rope;
+
+/* Q, K and V rows of the new tokens, bf16, heads of a token next to each other ([heads][d]); *_stride: elements between
+ * consecutive tokens (a multiple of 8, at least heads * d), so that all three may be views of one projection's rows.
+ * Addresses are 16-byte aligned. */
+typedef struct {
+    const void *q, *k, *v;      /* DEVICE; q may be NULL: K and V alone */
+    int64_t q_stride, k_stride, v_stride;
+} ampd_qkv_rows;
+
+/* Per (page, KV head) and channel the largest and the smallest stored key of the page's tokens, in 8 bits:
+ * largest <= codes[..][0][x] * scale, smallest >= codes[..][1][x] * scale, so that
+ * q.k <= sum_x (max(q_x, 0) codes[0][x] + min(q_x, 0) codes[1][x]) * scale for every key of the page.
+ * scale = 2^e, e = the smallest integer with amax <= 127 * 2^e (clamped to [-40, 96]; beyond it codes saturate at +-127);
+ * codes are rounded up (largest) and down (smallest).  Everything is exact in 32 bits: there is one right byte image. */
+typedef struct {
+    int8_t *codes;              /* DEVICE [num_pages][Hkv][2][d], 16-byte aligned */
+    float *scale;               /* DEVICE [num_pages][Hkv] */
+} ampd_page_bounds;
+
+/* Rotate q and k and append: q_out (DEVICE bf16 [sum L][Hq][d]) receives the rotated queries; it may be rows->q itself when
+ * q_stride = Hq * d, and overlaps no other argument otherwise.  The rotated keys, rounded to bf16, and v go into the pages as
+ * by ampd_kv_append, bit for bit, over both kinds of cache.  Keys are rotated in 64 bits and rounded to 32 and then to 16:
+ * one right byte image.  bounds: NULL, or the bounds of the pages that receive tokens are set as by ampd_page_bounds_update. */
+ampd_status ampd_rope_kv_append(const ampd_kv_cache *cache, const ampd_batch *batch, const ampd_rope *rope,
+                                const ampd_qkv_rows *rows, void *q_out, const ampd_page_bounds *bounds, void *stream);
+
+/* Set the bounds of every page that holds some of the tokens [C_r, C_r + L_r), from all its keys at positions < C_r + L_r. */
+ampd_status ampd_page_bounds_update(const ampd_kv_cache *cache, const ampd_batch *batch, const ampd_page_bounds *bounds,
+                                    void *stream);
+
+/* Queries are taken in groups of group_tokens consecutive new tokens of a request (its last group may have fewer); the
+ * groups of a batch are numbered request by request, request r having ceil(L_r / group_tokens).  Every group chooses pages of
+ * its request for each KV head. */
+typedef struct {
+    int32_t budget;             /* pages per group and KV head; >= first_pages + last_pages + ceil((group_tokens - 1) / P) */
+    int32_t first_pages;        /* the request's first pages are always chosen: >= 0 */
+    int32_t last_pages;         /* and the last ones up to the page of the group's first token (>= 1), and those up to its last token's */
+    int32_t group_tokens;       /* >= 1; group_tokens * (Hq / Hkv) <= 128 */
+    int32_t reserved[4];        /* must be 0 */
+} ampd_page_selection;
+
+/* selected: DEVICE int32 [groups][Hkv][budget]: logical page indices (into the request's block-table row), ascending, -1
+ * behind them when the request has fewer pages.  The pages that are not always chosen are taken by their score, the largest
+ * first and the lowest index among equals:
+ *   c = q / 2^f rounded to whole numbers, ties to even, f = the smallest integer with |q| <= 127 * 2^f over the group's queries
+ *       of the KV head's heads;
+ *   n = sum over channels x of (sum of max(c, 0) over the group) * codes[0][x] + (sum of min(c, 0)) * codes[1][x];
+ *   score = n rounded to 32-bit floating point, times the page's scale.
+ * n is a whole number below 2^31, so the choice does not depend on any order of summation.
+ * q: DEVICE bf16 [sum L][Hq][d], 16-byte aligned, finite.  The cache's pools are not read.
+ * workspace: DEVICE, 256-byte aligned, >= ampd_select_pages_workspace_bytes() (0: invalid arguments). */
+size_t ampd_select_pages_workspace_bytes(const ampd_kv_cache *cache, const ampd_batch *batch, const ampd_page_selection *sel);
+ampd_status ampd_select_pages(const ampd_kv_cache *cache, const ampd_batch *batch, const ampd_page_bounds *bounds,
+                              const ampd_page_selection *sel, const void *q, int32_t *selected, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* Attention of every new token over the keys at positions <= its own of the pages that its group's list names (the pools must
+ * already hold them).  selected: DEVICE int32 [groups][Hkv][budget] in any order; entries < 0 or behind the page of the
+ * group's last token are ignored, a page that is listed twice counts twice; a query that sees no key gets zeros.
+ * budget >= 1, group_tokens as above.  q, out: DEVICE bf16 [sum L][Hq][d], 16-byte aligned.
+ * workspace: DEVICE, 256-byte aligned, >= ampd_sparse_attn_workspace_bytes() (0: invalid arguments). */
+size_t ampd_sparse_attn_workspace_bytes(const ampd_kv_cache *cache, const ampd_batch *batch, int32_t budget, int32_t group_tokens);
+ampd_status ampd_sparse_attn(const ampd_kv_cache *cache, const ampd_batch *batch, const int32_t *selected, int32_t budget,
+                             int32_t group_tokens, const void *q, void *out, void *workspace, size_t workspace_bytes,
+                             void *stream);
+
 /* Description of the work list the planner builds for a batch from its (l_hist, l_incr)
  * metadata (host only; for tests and for the benchmark's roofline accounting).  Returns
  * AMPD_OK or a validation error. */

@@ -6,8 +6,10 @@ been built, importing the binding raises.
 """
 from .binding import (KVCache, kv_append, kv_pack, kv_unpack, incr_prefill_attn, mixed_batch_attn, paged_attn,
                       init, mixed_batch_attn_static, static_workspace_limit, workspace_bytes, plan_describe, plan_items, set_timing, last_timing,
-                      status_string, version, AmpdError, lib, LIB_PATH, EXPORTED_SYMBOLS)
+                      Rope, PageBounds, rope_kv_append, page_bounds_update, select_pages, select_pages_workspace_bytes, sparse_attn,
+                      sparse_attn_workspace_bytes, num_groups, status_string, version, AmpdError, lib, LIB_PATH, EXPORTED_SYMBOLS)
 
 __all__ = ["KVCache", "kv_append", "kv_pack", "kv_unpack", "incr_prefill_attn", "mixed_batch_attn", "paged_attn",
            "init", "mixed_batch_attn_static", "static_workspace_limit", "workspace_bytes", "plan_describe", "plan_items", "set_timing", "last_timing",
-           "status_string", "version", "AmpdError", "lib", "LIB_PATH", "EXPORTED_SYMBOLS"]
+           "Rope", "PageBounds", "rope_kv_append", "page_bounds_update", "select_pages", "select_pages_workspace_bytes", "sparse_attn",
+           "sparse_attn_workspace_bytes", "num_groups", "status_string", "version", "AmpdError", "lib", "LIB_PATH", "EXPORTED_SYMBOLS"]

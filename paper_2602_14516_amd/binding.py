@@ -22,6 +22,8 @@ EXPORTED_SYMBOLS = [
     "ampd_mixed_batch_attn_opts", "ampd_paged_attn", "ampd_plan_describe", "ampd_plan_items",
     "ampd_set_timing", "ampd_last_timing", "ampd_status_string", "ampd_version", "ampd_kv_pack", "ampd_kv_unpack",
     "ampd_init", "ampd_mixed_batch_attn_static", "ampd_static_workspace_limit",
+    "ampd_rope_kv_append", "ampd_page_bounds_update", "ampd_select_pages_workspace_bytes", "ampd_select_pages",
+    "ampd_sparse_attn_workspace_bytes", "ampd_sparse_attn",
 ]
 
 AMPD_KV_BF16, AMPD_KV_FP8_E4M3 = 0, 1
@@ -59,8 +61,25 @@ class _PlanInfo(ctypes.Structure):
                                               "partial_bytes", "plan_bytes", "num_append_items", "num_workgroups")]
 
 
+class _Rope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("inv_freq", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v")] + [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")]
+
+
+class _Bounds(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class _Selection(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("budget", "first_pages", "last_pages", "group_tokens")] + [("reserved", ctypes.c_int32 * 4)]
+
+
 HOST_ONLY_SYMBOLS = ["ampd_workspace_bytes", "ampd_workspace_bytes_opts", "ampd_plan_describe", "ampd_plan_items",
-                     "ampd_status_string", "ampd_version"]
+                     "ampd_status_string", "ampd_version", "ampd_select_pages_workspace_bytes", "ampd_sparse_attn_workspace_bytes"]
 
 
 class _HostOnly:
@@ -97,6 +116,12 @@ def _declare(f, cp, bp):
             ("ampd_plan_items", i64, [cp, bp, op, vp, i64]),
             ("ampd_set_timing", None, [ctypes.c_int]),
             ("ampd_last_timing", i32, [ctypes.POINTER(ctypes.c_float)] * 3),
+            ("ampd_rope_kv_append", i32, [cp, bp, vp, vp, vp, vp, vp]),
+            ("ampd_page_bounds_update", i32, [cp, bp, vp, vp]),
+            ("ampd_select_pages_workspace_bytes", sz, [cp, bp, vp]),
+            ("ampd_select_pages", i32, [cp, bp, vp, vp, vp, vp, vp, sz, vp]),
+            ("ampd_sparse_attn_workspace_bytes", sz, [cp, bp, i32, i32]),
+            ("ampd_sparse_attn", i32, [cp, bp, vp, i32, i32, vp, vp, vp, sz, vp]),
             ("ampd_status_string", ctypes.c_char_p, [i32]),
             ("ampd_version", ctypes.c_char_p, [])):
         fn = getattr(f, name)
@@ -223,7 +248,7 @@ def _batch_arg(ctx_len, incr_len, block_table_dev, block_table_host=None):
 # Calls with arguments of the usual kind go through an extension module (csrc/fastcall.cpp), which fills the two structures itself and
 # answers None, before anything is called, for the others; those take the functions below.  Once the smallest launches take 6.5 us on the
 # GPU, 3 us of interpreted marshalling in front of 4 us of library and launch kept them 7.9 us apart.
-_fastcall = None                 # (call, addresses of the entry points) after the first use; False: there is no such module
+_fastcall = None                 # (call, addresses of the entry points, module) after the first use; False: there is no such module
 
 
 def _load_fastcall():
@@ -243,7 +268,7 @@ def _load_fastcall():
                       "python paper_2602_14516_amd/build.py builds it", RuntimeWarning)
         return False
     module.streams(torch._C._cuda_getDevice, raw, torch._C._cuda_isInBadFork)
-    return module.call, {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in EXPORTED_SYMBOLS}
+    return module.call, {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in EXPORTED_SYMBOLS}, module
 
 
 def _fast(name, *args):
@@ -253,8 +278,18 @@ def _fast(name, *args):
         _fastcall = _load_fastcall()
     if not _fastcall:
         return None
-    call, address = _fastcall
+    call, address, _ = _fastcall
     return call(address[name], *args)
+
+
+def _fast_sparse(function, name, *args):
+    """The same through the module's function for an operator of sparse attention, which checks the tensors too."""
+    global _fastcall
+    if _fastcall is None:
+        _fastcall = _load_fastcall()
+    if not _fastcall:
+        return None
+    return getattr(_fastcall[2], function)(_fastcall[1][name], *args)
 
 
 def _opts(force_kv_splits=0):
@@ -429,6 +464,252 @@ def paged_attn(cache: KVCache, ctx_len, incr_len, block_table, q, *, out=None, w
     _check(_packed.ampd_paged_attn(c, b, _ptr(q), _ptr(out), _ptr(workspace),
                                workspace.numel() * workspace.element_size(), _stream_ptr(stream), o),
            "ampd_paged_attn")
+    return out
+
+
+# ---- sparse attention over a long cache ----------------------------------------------------------------------------------
+
+
+@dataclass
+class Rope:
+    """Position rotation: the inverse frequencies (torch, device, float32 [rotary_dim / 2]) and how elements are paired:
+    (j, j + rotary_dim / 2), or (2j, 2j + 1) when interleaved.  scale multiplies cosine and sine."""
+    inv_freq: object
+    interleaved: bool = False
+    scale: float = 1.0
+
+
+@dataclass
+class PageBounds:
+    """Per (page, KV head) the largest and smallest stored key of every channel in 8 bits: codes int8 [num_pages, Hkv, 2, d],
+    scale float32 [num_pages, Hkv] (torch, device)."""
+    codes: object
+    scale: object
+
+
+def _want(name, t, dtype, shape=None):
+    """Refuse a tensor that the library would read as something else: type, shape, order."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != getattr(torch, dtype):
+        raise ValueError(f"{name}: a torch tensor of {dtype} is wanted, not {getattr(t, 'dtype', type(t).__name__)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor is wanted (strides {tuple(t.stride())} for {tuple(t.shape)})")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: {tuple(shape)} is wanted, not {tuple(t.shape)}")
+
+
+def _same_device(named):
+    """The library enqueues on the current GPU: everything has to live there."""
+    import torch
+    dev = None
+    for name, t in named:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name}: device memory is wanted, not a tensor on {t.device}")
+        if dev is None:
+            dev = torch.cuda.current_device()
+        if t.device.index != dev:
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+
+
+def _want_table(block_table, rows):
+    _want("block_table", block_table, "int32")
+    if block_table.ndim != 2 or block_table.shape[0] != rows:
+        raise ValueError(f"block_table: one row for each of {rows} requests is wanted, not {tuple(block_table.shape)}")
+
+
+def _want_pools(cache: KVCache):
+    fp8 = cache.kv_dtype == AMPD_KV_FP8_E4M3
+    n = cache.k_pool.shape[0]
+    shape = (n, cache.num_kv_heads, cache.page_size, cache.head_dim)
+    for name, t in (("k_pool", cache.k_pool), ("v_pool", cache.v_pool)):
+        if t.element_size() != (1 if fp8 else 2) or not t.is_contiguous() or tuple(t.shape) != shape:
+            raise ValueError(f"{name}: {shape}, contiguous, {1 if fp8 else 2} bytes an element is wanted, not {tuple(t.shape)} of {t.dtype}")
+    if fp8:
+        _want("k_scale", cache.k_scale, "float32", (n, cache.num_kv_heads))
+        _want("v_scale", cache.v_scale, "float32", (n, cache.num_kv_heads))
+
+
+def _want_bounds(cache: KVCache, bounds: PageBounds):
+    n = cache.k_pool.shape[0] if cache.k_pool is not None else bounds.codes.shape[0]
+    _want("bounds.codes", bounds.codes, "int8", (n, cache.num_kv_heads, 2, cache.head_dim))
+    _want("bounds.scale", bounds.scale, "float32", (n, cache.num_kv_heads))
+
+
+def _rows(name, t, tokens, heads, d):
+    """[tokens, heads, d] with the heads of a token next to each other: elements from token to token."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or tuple(t.shape) != (tokens, heads, d):
+        raise ValueError(f"{name}: bfloat16 {(tokens, heads, d)} is wanted, not {getattr(t, 'dtype', type(t).__name__)} {tuple(getattr(t, 'shape', ()))}")
+    s = t.stride()
+    if tokens and (s[2] != 1 or heads > 1 and s[1] != d):
+        raise ValueError(f"{name}: the heads of a token have to lie next to each other (strides {tuple(s)})")
+    return max(int(s[0]), heads * d) if tokens < 2 else int(s[0])
+
+
+def _lengths(ctx_len, incr_len):
+    ctx, inc = np.ascontiguousarray(ctx_len, _INT32), np.ascontiguousarray(incr_len, _INT32)
+    if ctx.shape != inc.shape or ctx.ndim != 1:
+        raise ValueError(f"ctx_len and incr_len: two vectors of one length are wanted, not {ctx.shape} and {inc.shape}")
+    return ctx, inc
+
+
+def num_groups(incr_len, group_tokens=1) -> int:
+    """Groups of group_tokens consecutive new tokens that a batch has: rows of a selection."""
+    L = np.asarray(incr_len, dtype=np.int64)
+    return int((-(-L // int(group_tokens))).sum())
+
+
+def rope_kv_append(cache: KVCache, ctx_len, incr_len, block_table, rope: Rope, q, k_new, v_new, *, q_out=None, positions=None, bounds=None,
+                   stream=None, block_table_host=None):
+    """Rotate q and k_new by their positions and append k_new, v_new; returns the rotated queries (bf16 [sum L, Hq, d]).
+
+    q [sum L, Hq, d], k_new and v_new [sum L, Hkv, d] may be views of one projection's rows (a token's heads next to each other);
+    q None: keys and values alone.  q_out may be q where that is contiguous.  positions: int32 [sum L], device (None: token i of a
+    row is at ctx_len + i).  bounds: PageBounds, set for the pages that receive tokens."""
+    if q_out is not None and stream is None and block_table_host is None:
+        st = _fast_sparse("rope", "ampd_rope_kv_append", cache, ctx_len, incr_len, block_table, rope, q, k_new, v_new, q_out, positions, bounds)
+        if st is not None:
+            _check(st, "ampd_rope_kv_append")
+            return q_out
+    import torch
+    ctx, inc = _lengths(ctx_len, incr_len)
+    n = int(inc.sum())
+    _want_table(block_table, len(ctx))
+    _want_pools(cache)
+    d = cache.head_dim
+    _want("inv_freq", rope.inv_freq, "float32")
+    if rope.inv_freq.ndim != 1:
+        raise ValueError(f"inv_freq: a vector is wanted, not {tuple(rope.inv_freq.shape)}")
+    strides = [0 if q is None else _rows("q", q, n, cache.num_q_heads, d), _rows("k_new", k_new, n, cache.num_kv_heads, d),
+               _rows("v_new", v_new, n, cache.num_kv_heads, d)]
+    if positions is not None:
+        _want("positions", positions, "int32", (n,))
+    if bounds is not None:
+        _want_bounds(cache, bounds)
+    if q is not None and q_out is None:
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
+            q_out = torch.empty((n, cache.num_q_heads, d), dtype=torch.bfloat16, device=q.device)
+    if q is not None:
+        _want("q_out", q_out, "bfloat16", (n, cache.num_q_heads, d))
+    _same_device((("k_pool", cache.k_pool), ("v_pool", cache.v_pool), ("k_scale", cache.k_scale), ("v_scale", cache.v_scale),
+                  ("block_table", block_table), ("inv_freq", rope.inv_freq), ("q", q), ("k_new", k_new), ("v_new", v_new), ("q_out", q_out if q is not None else None),
+                  ("positions", positions), ("bounds", None if bounds is None else bounds.codes), ("bounds", None if bounds is None else bounds.scale)))
+    b, keep = _batch_arg(ctx, inc, block_table, block_table_host)
+    ro = _Rope(2 * rope.inv_freq.shape[0], int(bool(rope.interleaved)), _ptr(rope.inv_freq), _ptr(positions), float(rope.scale), 0)
+    rows = _Rows(_ptr(q), _ptr(k_new), _ptr(v_new), *strides)
+    bo = None if bounds is None else ctypes.byref(_Bounds(_ptr(bounds.codes), _ptr(bounds.scale)))
+    _check(_packed.ampd_rope_kv_append(_cache_arg(cache), b, ctypes.byref(ro), ctypes.byref(rows), None if q is None else _ptr(q_out), bo, _stream_ptr(stream)),
+           "ampd_rope_kv_append")
+    return q_out if q is not None else None
+
+
+def page_bounds_update(cache: KVCache, ctx_len, incr_len, block_table, bounds: PageBounds, *, stream=None, block_table_host=None) -> None:
+    """Set the bounds of every page that holds some of a row's tokens ctx_len .. ctx_len + incr_len, from the keys it stores."""
+    if stream is None and block_table_host is None:
+        st = _fast_sparse("page_bounds", "ampd_page_bounds_update", cache, ctx_len, incr_len, block_table, bounds)
+        if st is not None:
+            return _check(st, "ampd_page_bounds_update")
+    ctx, inc = _lengths(ctx_len, incr_len)
+    _want_table(block_table, len(ctx))
+    _want_pools(cache)
+    _want_bounds(cache, bounds)
+    _same_device((("k_pool", cache.k_pool), ("k_scale", cache.k_scale), ("block_table", block_table), ("bounds", bounds.codes), ("bounds", bounds.scale)))
+    b, keep = _batch_arg(ctx, inc, block_table, block_table_host)
+    _check(_packed.ampd_page_bounds_update(_cache_arg(cache), b, ctypes.byref(_Bounds(_ptr(bounds.codes), _ptr(bounds.scale))), _stream_ptr(stream)),
+           "ampd_page_bounds_update")
+
+
+def _selection(budget, first_pages, last_pages, group_tokens):
+    return _Selection(int(budget), int(first_pages), int(last_pages), int(group_tokens), (ctypes.c_int32 * 4)())
+
+
+def select_pages_workspace_bytes(cache: KVCache, ctx_len, incr_len, max_pages, budget, *, first_pages=1, last_pages=1, group_tokens=1) -> int:
+    b, keep = _batch(ctx_len, incr_len, None, max_pages=max_pages)
+    c = cache.c_struct()
+    s = _selection(budget, first_pages, last_pages, group_tokens)
+    return int(lib.ampd_select_pages_workspace_bytes(ctypes.byref(c), ctypes.byref(b), ctypes.byref(s)))
+
+
+def select_pages(cache: KVCache, ctx_len, incr_len, block_table, bounds: PageBounds, q, budget, *, first_pages=1, last_pages=1, group_tokens=1,
+                 out=None, workspace=None, stream=None, block_table_host=None):
+    """The `budget` pages of a row that every group of group_tokens new tokens attends, per KV head, chosen by their bounds: int32
+    [num_groups, Hkv, budget], logical page indices in ascending order, -1 behind.  The first first_pages, and the last last_pages up to
+    the group's own, are always among them.  q: the rotated queries, bf16 [sum L, Hq, d]."""
+    if out is not None and workspace is not None and stream is None and block_table_host is None:
+        st = _fast_sparse("select_pages", "ampd_select_pages", cache, ctx_len, incr_len, block_table, bounds, q, budget, first_pages, last_pages,
+                          group_tokens, out, workspace)
+        if st is not None:
+            _check(st, "ampd_select_pages")
+            return out
+    import torch
+    ctx, inc = _lengths(ctx_len, incr_len)
+    _want_table(block_table, len(ctx))
+    _want_bounds(cache, bounds)
+    _want("q", q, "bfloat16", (int(inc.sum()), cache.num_q_heads, cache.head_dim))
+    shape = (num_groups(inc, group_tokens), cache.num_kv_heads, int(budget))
+    if out is None:
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
+            out = torch.empty(shape, dtype=torch.int32, device=q.device)
+    _want("out", out, "int32", shape)
+    s = _selection(budget, first_pages, last_pages, group_tokens)
+    b, keep = _batch_arg(ctx, inc, block_table, block_table_host)
+    c = _selecting_cache(cache, bounds)
+    if workspace is None:
+        workspace = _temp_workspace(int(_packed.ampd_select_pages_workspace_bytes(c, b, ctypes.byref(s))), q, stream)
+    _same_device((("block_table", block_table), ("bounds", bounds.codes), ("bounds", bounds.scale), ("q", q), ("out", out), ("workspace", workspace)))
+    _check(_packed.ampd_select_pages(c, b, ctypes.byref(_Bounds(_ptr(bounds.codes), _ptr(bounds.scale))), ctypes.byref(s), _ptr(q), _ptr(out), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ampd_select_pages")
+    return out
+
+
+def _selecting_cache(cache: KVCache, bounds: PageBounds):
+    """The cache argument of a call that reads no pool: it may have none."""
+    if cache.k_pool is not None:
+        return _cache_arg(cache)
+    c = cache.c_struct()
+    c.num_pages = bounds.codes.shape[0]
+    return ctypes.byref(c)
+
+
+def sparse_attn_workspace_bytes(cache: KVCache, ctx_len, incr_len, max_pages, budget, *, group_tokens=1) -> int:
+    b, keep = _batch(ctx_len, incr_len, None, max_pages=max_pages)
+    c = cache.c_struct()
+    return int(lib.ampd_sparse_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(b), int(budget), int(group_tokens)))
+
+
+def sparse_attn(cache: KVCache, ctx_len, incr_len, block_table, selected, q, *, group_tokens=1, out=None, workspace=None, stream=None,
+                block_table_host=None):
+    """Attention of every new token over the keys up to its own position on the pages that its group's row of `selected` (int32 [num_groups,
+    Hkv, budget], as select_pages returns it) names; the pools must already hold all tokens.  Returns out (bf16 [sum L, Hq, d])."""
+    if out is not None and workspace is not None and stream is None and block_table_host is None:
+        st = _fast_sparse("sparse_attn", "ampd_sparse_attn", cache, ctx_len, incr_len, block_table, selected, q, group_tokens, out, workspace)
+        if st is not None:
+            _check(st, "ampd_sparse_attn")
+            return out
+    import torch
+    ctx, inc = _lengths(ctx_len, incr_len)
+    _want_table(block_table, len(ctx))
+    _want_pools(cache)
+    shape = (int(inc.sum()), cache.num_q_heads, cache.head_dim)
+    _want("q", q, "bfloat16", shape)
+    _want("selected", selected, "int32")
+    if selected.ndim != 3 or tuple(selected.shape[:2]) != (num_groups(inc, group_tokens), cache.num_kv_heads):
+        raise ValueError(f"selected: [{num_groups(inc, group_tokens)}, {cache.num_kv_heads}, budget] is wanted, not {tuple(selected.shape)}")
+    budget = int(selected.shape[2])
+    if out is None:
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
+            out = torch.empty_like(q)
+    _want("out", out, "bfloat16", shape)
+    b, keep = _batch_arg(ctx, inc, block_table, block_table_host)
+    c = _cache_arg(cache)
+    if workspace is None:
+        workspace = _temp_workspace(int(_packed.ampd_sparse_attn_workspace_bytes(c, b, budget, int(group_tokens))), q, stream)
+    _same_device((("k_pool", cache.k_pool), ("v_pool", cache.v_pool), ("k_scale", cache.k_scale), ("v_scale", cache.v_scale), ("block_table", block_table),
+                  ("selected", selected), ("q", q), ("out", out), ("workspace", workspace)))
+    _check(_packed.ampd_sparse_attn(c, b, _ptr(selected), budget, int(group_tokens), _ptr(q), _ptr(out), _ptr(workspace),
+                                    workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ampd_sparse_attn")
     return out
 
 

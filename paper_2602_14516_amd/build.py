@@ -6,8 +6,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libampd.so")
-SOURCES = ["kernels.hip", "api.cpp", "api_host.cpp", "plan.cpp"]
-HEADERS = ["kernels.h", "steps.h", "plan.h", "api_host.h", os.path.join(INCLUDE, "ampd.h")]
+SOURCES = ["kernels.hip", "sparse.hip", "api.cpp", "sparse_api.cpp", "api_host.cpp", "sparse_host.cpp", "plan.cpp"]
+KERNEL_SOURCES = [f for f in SOURCES if f.endswith(".hip")]
+HEADERS = ["kernels.h", "sparse.h", "steps.h", "plan.h", "api_host.h", os.path.join(INCLUDE, "ampd.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 
@@ -41,28 +42,30 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 
 def kernel_resources() -> dict:
-    """Registers, scratch and LDS of every kernel in kernels.hip, as the compiler reports them for gfx950
+    """Registers, scratch and LDS of every kernel, as the compiler reports them for gfx950
     (-Rpass-analysis=kernel-resource-usage; device code only, nothing is linked or written next to the sources)."""
     import re
     import tempfile
-    with tempfile.TemporaryDirectory() as tmp:
-        cmd = [HIPCC, "--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-               "-I", INCLUDE, "-I", CSRC, "-c", "--cuda-device-only", "-Rpass-analysis=kernel-resource-usage",
-               os.path.join(CSRC, "kernels.hip"), "-o", os.path.join(tmp, "kernels.o")]
-        res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stdout)
-    out, name = {}, None
-    for line in res.stdout.splitlines():
-        m = re.search(r"remark:\s+(Function Name|VGPRs|AGPRs|TotalSGPRs|ScratchSize \[bytes/lane\]|VGPRs Spill|SGPRs Spill|"
-                      r"LDS Size \[bytes/block\]|Occupancy \[waves/SIMD\]): (\S+)", line)
-        if not m:
-            continue
-        if m.group(1) == "Function Name":
-            name = m.group(2)
-            out[name] = {}
-        elif name is not None:
-            out[name][m.group(1)] = int(m.group(2))
+    out = {}
+    for src in KERNEL_SOURCES:
+        with tempfile.TemporaryDirectory() as tmp:
+            cmd = [HIPCC, "--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+                   "-I", INCLUDE, "-I", CSRC, "-c", "--cuda-device-only", "-Rpass-analysis=kernel-resource-usage",
+                   os.path.join(CSRC, src), "-o", os.path.join(tmp, "kernels.o")]
+            res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stdout)
+        name = None
+        for line in res.stdout.splitlines():
+            m = re.search(r"remark:\s+(Function Name|VGPRs|AGPRs|TotalSGPRs|ScratchSize \[bytes/lane\]|VGPRs Spill|SGPRs Spill|"
+                          r"LDS Size \[bytes/block\]|Occupancy \[waves/SIMD\]): (\S+)", line)
+            if not m:
+                continue
+            if m.group(1) == "Function Name":
+                name = m.group(2)
+                out[name] = {}
+            elif name is not None:
+                out[name][m.group(1)] = int(m.group(2))
     return out
 
 
@@ -112,7 +115,7 @@ def build_host_sanitized(address: bool = True):
     san = "address,undefined" if address else "undefined"
     flags = ["g++", "-O1", "-g", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-fsanitize={san}",
              "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer", "-I", INCLUDE, "-I", CSRC]
-    subprocess.check_call(flags + [os.path.join(CSRC, "api_host.cpp"), os.path.join(CSRC, "plan.cpp"), "-o", HOST_SAN_LIB])
+    subprocess.check_call(flags + [os.path.join(CSRC, f) for f in ("api_host.cpp", "sparse_host.cpp", "plan.cpp")] + ["-o", HOST_SAN_LIB])
     subprocess.check_call(flags + [SCHED_SRC, "-o", SCHED_SAN_LIB])
     runtime = None
     if address:

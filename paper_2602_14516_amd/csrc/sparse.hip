@@ -1,0 +1,1244 @@
+// HIP kernels for gfx950 of sparse attention over a paged KV cache: rotate and append, page bounds, page selection, attention over the
+// selected pages (the steps of a block of 32 keys are those of the dense kernels, see kernels.hip).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "sparse.h"
+#include "steps.h"
+
+namespace ampd {
+
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------------------------------------
+// page bounds
+
+// Chunks of 8 elements of a key are handled in pairs, D / 16 to a key: unit u of a page is slot u / (D / 16), pair u % (D / 16), and a lane
+// whose units are 64 apart keeps its pair.
+template <int D>
+struct Units {
+    static constexpr int PPT = D / 16;                // pairs per token
+    static constexpr int COUNT(int P) { return P * PPT / 64; }
+};
+
+__device__ __forceinline__ void unpack8(const u32x4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void decode8(uint32_t lo, uint32_t hi, float (&f)[8]) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(lo, true);
+    const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
+}
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+    return x;
+}
+
+// The lane's largest and smallest values so far of its 16 channels (chunk a: 0..7, chunk b: 8..15), over its own units.
+struct LaneBounds {
+    float hi[16], lo[16];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            hi[i] = NEG_INF;
+            lo[i] = -NEG_INF;
+        }
+    }
+    __device__ __forceinline__ void take(int at, const float (&f)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            hi[at + i] = fmaxf(hi[at + i], f[i]);
+            lo[at + i] = fminf(lo[at + i], f[i]);
+        }
+    }
+};
+
+// Half of the N values that the lane holds go to the lane `bit` away, which sends the other half: what stays is over both lanes.
+template <int N>
+__device__ __forceinline__ void exchange(float (&hi)[16], float (&lo)[16], int bit, bool upper) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const float h = __shfl_xor(upper ? hi[i] : hi[N / 2 + i], bit, 64), l = __shfl_xor(upper ? lo[i] : lo[N / 2 + i], bit, 64);
+        hi[i] = fmaxf(upper ? hi[N / 2 + i] : hi[i], h);
+        lo[i] = fminf(upper ? lo[N / 2 + i] : lo[i], l);
+    }
+}
+
+// smallest e with amax <= 127 * 2^e  (127 = 1.984375 * 2^6), clamped to [-40, 96]
+__device__ __forceinline__ int bounds_exponent(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    const int ex = (int)(u >> 23) - 127;
+    int e = (u & 0x7fffffu) <= 0x7e0000u ? ex - 6 : ex - 5;
+    if ((u >> 23) == 0) e = -40;                      // zero / subnormal
+    return min(96, max(-40, e));
+}
+
+// Bounds of a page of one KV head from the wave's lanes; unit: what the lanes' values count in (a power of two: an 8-bit page's scale).
+// The lanes that share a pair of chunks halve their values log2(64 / (D / 16)) times, so that 28 exchanges do instead of 96.
+template <int D>
+__device__ __forceinline__ void store_bounds(LaneBounds& b, float unit, int ca, int cb, int lane, int8_t* codes, float* scale) {
+    exchange<16>(b.hi, b.lo, 32, lane & 32);
+    exchange<8>(b.hi, b.lo, 16, lane & 16);
+    exchange<4>(b.hi, b.lo, 8, lane & 8);
+    if constexpr (D == 64) exchange<2>(b.hi, b.lo, 4, lane & 4);
+    constexpr int N = D == 64 ? 1 : 2;                // neighbouring channels that the lane is left with
+    const int x = (lane & 32 ? cb : ca) * 8 + (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0) + (D == 64 && (lane & 4) ? 1 : 0);
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        b.hi[i] *= unit;
+        b.lo[i] *= unit;
+        amax = fmaxf(amax, fmaxf(fabsf(b.hi[i]), fabsf(b.lo[i])));
+    }
+    const int e = bounds_exponent(wave_max(amax));
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    int8_t h[N], l[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        // (a value that underflows when it is scaled still counts)
+        float u = ceilf(b.hi[i] * inv), d = floorf(b.lo[i] * inv);
+        if (b.hi[i] > 0.0f) u = fmaxf(u, 1.0f);
+        if (b.lo[i] < 0.0f) d = fminf(d, -1.0f);
+        h[i] = (int8_t)(int)fminf(fmaxf(u, -127.0f), 127.0f);
+        l[i] = (int8_t)(int)fminf(fmaxf(d, -127.0f), 127.0f);
+    }
+    if constexpr (N == 2) {
+        *reinterpret_cast<uint16_t*>(codes + x) = (uint16_t)((uint8_t)h[0] | (uint8_t)h[1] << 8);
+        *reinterpret_cast<uint16_t*>(codes + D + x) = (uint16_t)((uint8_t)l[0] | (uint8_t)l[1] << 8);
+    } else {
+        codes[x] = h[0];
+        codes[D + x] = l[0];
+    }
+    if (lane == 0) *scale = __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// A wave per page and KV head.
+template <int D, int P, int KVT>
+__global__ __launch_bounds__(WG) void page_bounds_kernel(const BoundsParams p) {
+    constexpr int PPT = Units<D>::PPT, NU = Units<D>::COUNT(P);
+    const int lane = threadIdx.x & 63, h = blockIdx.y * (WG / 64) + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const PageJob j = page_job(p.a);
+    if (h >= p.a.Hkv || (uint32_t)j.page >= (uint64_t)p.num_pages) return;
+    const int slots = j.t1 - (j.t0 & ~(P - 1)), pair = lane % PPT;
+    const int64_t ph = (int64_t)j.page * p.a.Hkv + h;
+    const char* pg = static_cast<const char*>(p.a.k_pool) + ph * (P * D * (KVT == KV_FP8 ? 1 : 2));
+    float unit = 1.0f;
+    if constexpr (KVT == KV_FP8) unit = p.a.k_scale[ph];
+    LaneBounds b;
+    b.clear();
+    u32x4 x[NU], y[NU];
+#pragma unroll
+    for (int k = 0; k < NU; ++k) {
+        const int s = min((lane + 64 * k) / PPT, slots - 1);              // (a slot behind the last token: the last token's once more)
+        if constexpr (KVT == KV_BF16) {
+            x[k] = *reinterpret_cast<const u32x4*>(pg + s * (D * 2) + pair * 16);
+            y[k] = *reinterpret_cast<const u32x4*>(pg + s * (D * 2) + (pair + PPT) * 16);
+        } else {
+            x[k] = *reinterpret_cast<const u32x4*>(pg + s * D + pair * 16);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < NU; ++k) {
+        float f[8];
+        if constexpr (KVT == KV_BF16) {
+            unpack8(x[k], f);
+            b.take(0, f);
+            unpack8(y[k], f);
+            b.take(8, f);
+        } else {
+            decode8(x[k].x, x[k].y, f);
+            b.take(0, f);
+            decode8(x[k].z, x[k].w, f);
+            b.take(8, f);
+        }
+    }
+    const int ca = KVT == KV_BF16 ? pair : 2 * pair, cb = KVT == KV_BF16 ? pair + PPT : 2 * pair + 1;
+    store_bounds<D>(b, unit, ca, cb, lane, p.codes + ph * (2 * D), p.bscale + ph);
+}
+
+// ---------------------------------------------------------------------------------------------
+// rotate and append
+
+// The chunks of a pair: while rotated elements remain, two chunks whose elements the rotation pairs (half apart) or two chunks of
+// neighbouring pairs (interleaved); behind them two neighbouring chunks that are copied.
+struct ChunkPair {
+    int a, b;
+    bool rotated;
+};
+__device__ __forceinline__ ChunkPair chunk_pair(int pair, int rd) {
+    const int half = rd >> 4;
+    if (pair < half) return {pair, pair + half, true};
+    return {2 * pair, 2 * pair + 1, false};           // (rd / 8 + 2 (pair - rd / 16))
+}
+
+// Rotate a pair of chunks in type F; cs(i): cosine and sine of the i-th of the 8 angles of the pair (half apart: those of elements 0..7;
+// interleaved: of the 4 pairs of chunk a, then of chunk b).
+template <class F, class CS>
+__device__ __forceinline__ void rotate(u32x4& va, u32x4& vb, bool interleaved, CS&& cs) {
+    float a[8], b[8];
+    unpack8(va, a);
+    unpack8(vb, b);
+    bf16x8 ra, rb;
+    auto turn = [&](int i, float x1, float x2, __bf16& y1, __bf16& y2) {
+        F c, s;
+        cs(i, c, s);
+        float f1 = (float)((F)x1 * c - (F)x2 * s), f2 = (float)((F)x2 * c + (F)x1 * s);
+        // two roundings, as defined: the compiler would make one of 64 -> 32 -> 16 bits (it differs where 32 bits end on a tie, 4 of a million)
+        if constexpr (sizeof(F) == 8) asm("" : "+v"(f1), "+v"(f2));
+        y1 = (__bf16)f1;
+        y2 = (__bf16)f2;
+    };
+    if (interleaved) {                                // uniform
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __bf16 y1, y2;
+            turn(i, a[2 * i], a[2 * i + 1], y1, y2);
+            ra[2 * i] = y1;
+            ra[2 * i + 1] = y2;
+            turn(4 + i, b[2 * i], b[2 * i + 1], y1, y2);
+            rb[2 * i] = y1;
+            rb[2 * i + 1] = y2;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            __bf16 y1, y2;
+            turn(i, a[i], b[i], y1, y2);
+            ra[i] = y1;
+            rb[i] = y2;
+        }
+    }
+    va = __builtin_bit_cast(u32x4, ra);
+    vb = __builtin_bit_cast(u32x4, rb);
+}
+
+// One workgroup column per page that new tokens fall into; the column's waves share its jobs: K of a head, V of a head (the page's new tokens
+// in registers, with the cached ones where the page's scale or bounds need them), and runs of 256 pairs of chunks of Q.
+// The angles' cosines and sines are computed once per workgroup, in 64 bits, and kept as two 32-bit parts each: Q is rotated by the
+// first, K by both, in 64 bits (K decides 8-bit codes, scales, bounds and through them page choices, which are whole numbers).
+template <int D, int P, int KVT, bool BOUNDS>
+__global__ __launch_bounds__(WG) void rope_append_kernel(const RopeParams p) {
+    constexpr int PPT = Units<D>::PPT, NU = Units<D>::COUNT(P), ES = KVT == KV_FP8 ? 1 : 2;
+    __shared__ f32x2 head[P * D / 2], tail[P * D / 2];                // (cos, sin) of token t, angle i at t * rd / 2 + i
+    const AppendParams& a = p.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const PageJob j = page_job(a);
+    const int n = j.t1 - j.t0, s0 = j.t0 & (P - 1), F = p.rd >> 1;
+    for (int i = threadIdx.x; i < n * F; i += WG) {
+        const int t = i / F;
+        const int pos = p.positions ? p.positions[j.row + t] : j.t0 + t;
+        double s, c;
+        sincos((double)pos * (double)p.inv_freq[i - t * F], &s, &c);
+        c *= (double)p.scale;
+        s *= (double)p.scale;
+        const f32x2 top = {(float)c, (float)s};
+        head[i] = top;
+        tail[i] = f32x2{(float)(c - (double)top.x), (float)(s - (double)top.y)};
+    }
+    __syncthreads();
+    const int nkv = (uint32_t)j.page < (uint64_t)p.num_pages ? 2 * a.Hkv : 0, nq = p.q ? (n * p.Hq * PPT + 255) / 256 : 0;
+    const ChunkPair cp = chunk_pair(lane % PPT, p.rd);
+    // the i-th angle of the lane's pair, in table order
+    const int f0 = p.interleaved ? 4 * cp.a : 8 * cp.a, f1 = p.interleaved ? 4 * cp.b - 4 : f0;   // angles 0..3 from f0, 4..7 from f1
+    for (int job = blockIdx.y * (WG / 64) + wave; job < nkv + nq; job += gridDim.y * (WG / 64)) {
+        if (job >= nkv) {
+            const int units = n * p.Hq * PPT, u0 = (job - nkv) * 256 + lane;
+            const float inv = __builtin_amdgcn_rcpf((float)p.Hq);
+            u32x4 x[4], y[4];
+            int tok[4], at[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int u = min(u0 + 64 * k, units - 1), th = u / PPT;
+                tok[k] = (int)(((float)th + 0.5f) * inv);                     // th / Hq: th < 2^20, Hq < 2^14
+                at[k] = th - tok[k] * p.Hq;
+                const char* src = static_cast<const char*>(p.q) + (int64_t)(j.row + tok[k]) * p.q_stride + at[k] * (D * 2);
+                x[k] = *reinterpret_cast<const u32x4*>(src + cp.a * 16);
+                y[k] = *reinterpret_cast<const u32x4*>(src + cp.b * 16);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (cp.rotated) {
+                    const f32x2* t = head + tok[k] * F;
+                    rotate<float>(x[k], y[k], p.interleaved, [&](int i, float& c, float& s) {
+                        const f32x2 v = t[(i < 4 ? f0 : f1) + i];
+                        c = v.x;
+                        s = v.y;
+                    });
+                }
+                if (u0 + 64 * k < units) {
+                    char* dst = static_cast<char*>(p.q_out) + ((int64_t)(j.row + tok[k]) * p.Hq + at[k]) * (D * 2);
+                    *reinterpret_cast<u32x4*>(dst + cp.a * 16) = x[k];
+                    *reinterpret_cast<u32x4*>(dst + cp.b * 16) = y[k];
+                }
+            }
+            continue;
+        }
+        const bool is_v = job >= a.Hkv;
+        const int h = is_v ? job - a.Hkv : job;
+        const int64_t ph = (int64_t)j.page * a.Hkv + h;
+        const char* src = static_cast<const char*>(is_v ? a.v_new : a.k_new) + (int64_t)j.row * (is_v ? p.v_stride : p.k_stride) + h * (D * 2);
+        const int64_t stride = is_v ? p.v_stride : p.k_stride;
+        char* pg = static_cast<char*>(is_v ? a.v_pool : a.k_pool) + ph * (P * D * ES);
+        const bool cached = s0 > 0 && (KVT == KV_FP8 || (BOUNDS && !is_v));
+        float* scl = KVT == KV_FP8 ? (is_v ? a.v_scale : a.k_scale) + ph : nullptr;
+        float s_old = 1.0f;
+        if (KVT == KV_FP8 && s0 > 0) s_old = *scl;
+        float unit = 1.0f;
+        LaneBounds lb;
+        if (BOUNDS) lb.clear();
+        // Units in runs: over a bf16 cache each run is done with before the next, so that a page of 64 tokens takes no more registers than one
+        // of 32; 8-bit pages need all new tokens' magnitudes first.
+        constexpr int RUN = KVT == KV_FP8 ? NU : NU < 4 ? NU : 4;
+#pragma unroll 1
+        for (int k0 = 0; k0 < NU; k0 += RUN) {
+            u32x4 x[RUN], y[RUN];
+            const int base = lane + 64 * k0;
+#pragma unroll
+            for (int k = 0; k < RUN; ++k) {
+                const int s = (base + 64 * k) / PPT;
+                x[k] = y[k] = u32x4{0, 0, 0, 0};
+                if (s >= s0 && s < s0 + n) {
+                    const char* r = src + (s - s0) * stride;
+                    x[k] = *reinterpret_cast<const u32x4*>(r + cp.a * 16);
+                    y[k] = *reinterpret_cast<const u32x4*>(r + cp.b * 16);
+                } else if (cached && s < s0) {
+                    if constexpr (KVT == KV_BF16) {
+                        x[k] = *reinterpret_cast<const u32x4*>(pg + (s * D + cp.a * 8) * 2);
+                        y[k] = *reinterpret_cast<const u32x4*>(pg + (s * D + cp.b * 8) * 2);
+                    } else {
+                        const u32x2 ca = *reinterpret_cast<const u32x2*>(pg + s * D + cp.a * 8), cb = *reinterpret_cast<const u32x2*>(pg + s * D + cp.b * 8);
+                        x[k] = u32x4{ca.x, ca.y, cb.x, cb.y};
+                    }
+                }
+            }
+            if (!is_v && cp.rotated) {
+#pragma unroll
+                for (int k = 0; k < RUN; ++k) {
+                    const int s = (base + 64 * k) / PPT;
+                    if (s >= s0 && s < s0 + n) {
+                        const int t = (s - s0) * F;
+                        rotate<double>(x[k], y[k], p.interleaved, [&](int i, double& c, double& sn) {
+                            const f32x2 v = head[t + (i < 4 ? f0 : f1) + i], w = tail[t + (i < 4 ? f0 : f1) + i];
+                            c = (double)v.x + (double)w.x;
+                            sn = (double)v.y + (double)w.y;
+                        });
+                    }
+                    __builtin_amdgcn_sched_barrier(0);                    // (one unit at a time: registers)
+                }
+            }
+            if constexpr (KVT == KV_FP8) {
+                float amax = 0.0f;
+#pragma unroll
+                for (int k = 0; k < RUN; ++k) {
+                    const int s = (base + 64 * k) / PPT;
+                    if (s >= s0) amax = fmaxf(amax, fmaxf(chunk_amax(x[k]), chunk_amax(y[k])));
+                }
+                int e = exponent_for(wave_max(amax));
+                const int e_old = (int)(__float_as_uint(s_old) >> 23) - 127;
+                const bool raise = s0 > 0 && e > e_old;
+                if (s0 > 0 && !raise) e = e_old;
+                const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+                const float f = __uint_as_float((uint32_t)(e_old - e + 127) << 23);     // (used where the exponent rises: 2^(e_old - e))
+#pragma unroll
+                for (int k = 0; k < RUN; ++k) {
+                    const int s = (base + 64 * k) / PPT;
+                    const bool fresh = s >= s0;
+                    if (fresh) {
+                        const u32x2 ca = encode_chunk(x[k], inv), cb = encode_chunk(y[k], inv);
+                        x[k] = u32x4{ca.x, ca.y, cb.x, cb.y};
+                    } else if (raise) {
+                        float g[8];
+                        decode8(x[k].x, x[k].y, g);
+                        x[k].x = encode4(g[0] * f, g[1] * f, g[2] * f, g[3] * f);
+                        x[k].y = encode4(g[4] * f, g[5] * f, g[6] * f, g[7] * f);
+                        decode8(x[k].z, x[k].w, g);
+                        x[k].z = encode4(g[0] * f, g[1] * f, g[2] * f, g[3] * f);
+                        x[k].w = encode4(g[4] * f, g[5] * f, g[6] * f, g[7] * f);
+                    }
+                    if (s < s0 + n && (fresh || raise)) {
+                        *reinterpret_cast<u32x2*>(pg + s * D + cp.a * 8) = u32x2{x[k].x, x[k].y};
+                        *reinterpret_cast<u32x2*>(pg + s * D + cp.b * 8) = u32x2{x[k].z, x[k].w};
+                    }
+                }
+                unit = __uint_as_float((uint32_t)(e + 127) << 23);
+                if (lane == 0) *scl = unit;
+            } else {
+#pragma unroll
+                for (int k = 0; k < RUN; ++k) {
+                    const int s = (base + 64 * k) / PPT;
+                    if (s >= s0 && s < s0 + n) {
+                        *reinterpret_cast<u32x4*>(pg + (s * D + cp.a * 8) * 2) = x[k];
+                        *reinterpret_cast<u32x4*>(pg + (s * D + cp.b * 8) * 2) = y[k];
+                    }
+                }
+            }
+            if constexpr (BOUNDS) {
+                if (!is_v) {
+#pragma unroll
+                    for (int k = 0; k < RUN; ++k) {
+                        if ((base + 64 * k) / PPT >= s0 + n) continue;
+                        float f[8];
+                        if constexpr (KVT == KV_BF16) {
+                            unpack8(x[k], f);
+                            lb.take(0, f);
+                            unpack8(y[k], f);
+                            lb.take(8, f);
+                        } else {
+                            decode8(x[k].x, x[k].y, f);
+                            lb.take(0, f);
+                            decode8(x[k].z, x[k].w, f);
+                            lb.take(8, f);
+                        }
+                    }
+                }
+            }
+        }
+        if constexpr (BOUNDS) {
+            if (!is_v) store_bounds<D>(lb, unit, cp.a, cp.b, lane, p.codes + ph * (2 * D), p.bscale + ph);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// page selection
+
+// Which row of a launch owns item idx: the last one that starts at or before it.
+template <class P, class F>
+__device__ __forceinline__ int row_of(const P& p, int max_rows, int idx, F&& start) {
+    const int lane = threadIdx.x & 63;
+    int r = -1;
+    for (int base = 0; base < max_rows && base < p.n; base += 64)
+        r += __popcll(__ballot(base + lane < p.n && start(p.rows[min(base + lane, p.n - 1)]) <= idx));
+    return __builtin_amdgcn_readfirstlane(r);
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t add_dpp(uint32_t x) {
+    return x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+// the sum over the 16 lanes of a row, in all of them
+__device__ __forceinline__ uint32_t row_sum(uint32_t x) {
+    x = add_dpp<0xB1>(x);                             // quad_perm [1, 0, 3, 2]
+    x = add_dpp<0x4E>(x);                             // quad_perm [2, 3, 0, 1]
+    x = add_dpp<0x124>(x);                            // row_ror:4
+    return add_dpp<0x128>(x);                         // row_ror:8
+}
+
+// Whole numbers of a group's queries for one KV head, summed over its rows (tokens x heads), as two limbs of 7 bits in the operand layout of
+// the 16x16x64 product: lane l holds bytes 16 (l / 16) .. of k-block kk; k = 0..d-1 the sums of the positive parts, d..2d-1 of the
+// negative ones.  Every lane of a row of 16 ends up with the same.  At most 128 rows of at most 127 each: sums below 2^14.
+template <int D>
+__device__ __forceinline__ void quantise_queries(const char* q, int64_t token_bytes, int G, int rows, int lane, i32x4 (&limb)[2][D / 32]) {
+    constexpr int NB = D / 64;                        // 64-channel blocks
+    const int col = lane & 15, c = lane >> 4;
+    auto load = [&](int r, int blk, u32x4& lo, u32x4& hi) {
+        const int t = r / G;
+        const char* src = q + t * token_bytes + (r - t * G) * (D * 2) + (blk * 64 + c * 16) * 2;
+        lo = *reinterpret_cast<const u32x4*>(src);
+        hi = *reinterpret_cast<const u32x4*>(src + 16);
+    };
+    float amax = 0.0f;
+    for (int r = col; r < rows; r += 16) {
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) {
+            u32x4 lo, hi;
+            load(r, blk, lo, hi);
+            amax = fmaxf(amax, fmaxf(chunk_amax(lo), chunk_amax(hi)));
+        }
+    }
+    amax = wave_max(amax);
+    // f: smallest with amax <= 127 * 2^f; a group of zeros: any
+    const uint32_t u = __float_as_uint(amax);
+    const int ex = (int)(u >> 23) - 127, f = (u & 0x7fffffu) <= 0x7e0000u ? ex - 6 : ex - 5;
+    const int fs = max(-126, min(127, -f));           // 2^-f in two factors: f reaches -138 and 122
+    const float m0 = __uint_as_float((uint32_t)(fs + 127) << 23), m1 = __uint_as_float((uint32_t)(max(-126, min(127, -f - fs)) + 127) << 23);
+    uint32_t sum[NB][16];                             // positive | negative << 16
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[blk][i] = 0;
+    for (int r = col; r < rows; r += 16) {
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) {
+            u32x4 lo, hi;
+            load(r, blk, lo, hi);
+            float v[8];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                unpack8(half ? hi : lo, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int x = (int)fminf(fmaxf(rintf(v[i] * m0 * m1), -127.0f), 127.0f);
+                    sum[blk][half * 8 + i] += x >= 0 ? (uint32_t)x : (uint32_t)(-x) << 16;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            uint32_t pl = 0, ph = 0, nl = 0, nh = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t s = row_sum(sum[blk][w * 4 + i]), pos = s & 0xffff, neg = s >> 16;
+                pl |= (pos & 127) << (8 * i);
+                ph |= (pos >> 7) << (8 * i);
+                nl |= ((0u - (neg & 127)) & 0xff) << (8 * i);
+                nh |= ((0u - (neg >> 7)) & 0xff) << (8 * i);
+            }
+            limb[0][blk][w] = (int)pl;
+            limb[1][blk][w] = (int)ph;
+            limb[0][NB + blk][w] = (int)nl;
+            limb[1][NB + blk][w] = (int)nh;
+        }
+    }
+}
+
+// A wave per group and KV head: the operand bytes, for the score launch's tiles of 16 groups.
+template <int D>
+__global__ __launch_bounds__(64) void query_codes_kernel(const SelectParams p) {
+    const int lane = threadIdx.x, item = blockIdx.x, h = blockIdx.y, G = p.Hq / p.Hkv;
+    const SelectRow r = p.rows[row_of(p, SELECT_MAX_REQS, item, [](const SelectRow& x) { return x.item0; })];
+    const int tok0 = (item - r.item0) * p.g, m = min(p.g, r.L - tok0);
+    const char* q = static_cast<const char*>(p.q) + ((int64_t)(r.row_off + tok0) * p.Hq + h * G) * (D * 2);
+    i32x4 limb[2][D / 32];
+    quantise_queries<D>(q, (int64_t)p.Hq * D * 2, G, m * G, lane, limb);
+    if ((lane & 15) == 0) {
+        int8_t* dst = p.qcodes + ((int64_t)item * p.Hkv + h) * (4 * D) + (lane >> 4) * 16;
+#pragma unroll
+        for (int l = 0; l < 2; ++l)
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk) *reinterpret_cast<i32x4*>(dst + l * (2 * D) + kk * 64) = limb[l][kk];
+    }
+}
+
+// Scores as 32-bit numbers that order as the scores do.
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// Scores of 16 groups x 16 pages at a time: the 16x16x64 whole-number product with the groups' queries as one operand and the pages' bounds
+// as the other (both with k = 0..2d-1: largest, then smallest), once per limb.  A wave goes through SCORE_TILES tiles of one KV head; the
+// waves of a workgroup are neighbouring heads of the same pages (a page's bounds of all heads lie next to each other), then
+// neighbouring pages.  ONE: every row of the launch has one group, whose queries the wave quantises itself.
+template <int D, bool ONE>
+__global__ __launch_bounds__(64 * SCORE_WAVES) void page_scores_kernel(const SelectParams p, int heads) {
+    constexpr int KK = D / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const SelectRow r = p.rows[row_of(p, SELECT_MAX_REQS, blockIdx.x, [](const SelectRow& x) { return x.tile0; })];
+    const int G = p.Hq / p.Hkv, per_wg = SCORE_TILES * 16 * (SCORE_WAVES / heads);
+    const int h = blockIdx.y * heads + wave % heads;
+    const int ng = (r.L + p.g - 1) / p.g, tiles = (ng + 15) >> 4, at = blockIdx.x - r.tile0, tile = at % tiles, block = at / tiles;
+    if (h >= p.Hkv) return;
+    // pages that the tile's last group may choose by score
+    const int last_group = min(ng, tile * 16 + 16) - 1;
+    const int end = ((r.C + last_group * p.g) >> p.logP) - p.last + 1;
+    const int pg0 = block * per_wg + (wave / heads) * (SCORE_TILES * 16);
+    if (pg0 >= end) return;
+    const int32_t* bt = p.block_table + (int64_t)r.req * p.max_pages;
+    const int col = lane & 15, c = lane >> 4;
+    int id[SCORE_TILES];
+#pragma unroll
+    for (int t = 0; t < SCORE_TILES; ++t) {
+        id[t] = bt[min(pg0 + t * 16 + col, end - 1)];
+        if ((uint32_t)id[t] >= (uint64_t)p.num_pages) id[t] = 0;
+    }
+    i32x4 limb[2][KK];
+    if constexpr (ONE) {
+        quantise_queries<D>(static_cast<const char*>(p.q) + ((int64_t)r.row_off * p.Hq + h * G) * (D * 2), (int64_t)p.Hq * D * 2, G, r.L * G, lane, limb);
+        if (col != 0) {
+#pragma unroll
+            for (int l = 0; l < 2; ++l)
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) limb[l][kk] = i32x4{0, 0, 0, 0};
+        }
+    } else {
+        const int item = r.item0 + min(tile * 16 + col, ng - 1);        // (a group behind the last: the last one's, not stored)
+        const int8_t* src = p.qcodes + ((int64_t)item * p.Hkv + h) * (4 * D) + c * 16;
+#pragma unroll
+        for (int l = 0; l < 2; ++l)
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) limb[l][kk] = *reinterpret_cast<const i32x4*>(src + l * (2 * D) + kk * 64);
+    }
+    const int64_t stride = (((int64_t)r.C + r.L + p.P - 1) / p.P + 63) / 64 * 64;
+    uint32_t* keys = p.keys + (int64_t)r.key0 * 64 + h * stride;
+#pragma unroll
+    for (int t = 0; t < SCORE_TILES; ++t) {
+        const int64_t ph = (int64_t)id[t] * p.Hkv + h;
+        const int8_t* src = p.codes + ph * (2 * D) + c * 16;
+        i32x4 b[KK];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) b[kk] = *reinterpret_cast<const i32x4*>(src + kk * 64);
+        const float scale = p.bscale[ph];
+        i32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(limb[0][kk], b[kk], lo, 0, 0, 0);
+            hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(limb[1][kk], b[kk], hi, 0, 0, 0);
+        }
+        const int page = pg0 + t * 16 + col;
+#pragma unroll
+        for (int i = 0; i < (ONE ? 1 : 4); ++i) {
+            const int g = ONE ? 0 : tile * 16 + c * 4 + i;
+            if (page < end && (ONE ? c == 0 : g < ng))
+                keys[(int64_t)g * p.Hkv * stride + page] = ordered((float)(hi[i] * 128 + lo[i]) * scale);
+        }
+    }
+}
+
+// Of n keys the `need` largest, the lowest index among equals, for one group and KV head; then the list in ascending order.
+// The keys' range is cut into 2 048 bins that are counted; the bin in which the need-th largest lies is cut again while it holds more than
+// LIST keys, whose ranks among themselves settle it otherwise.  (Bins of the leading bits would hold nearly everything in one: scores
+// of one row have few exponents.)  KPT keys per thread stay in registers; KPT = 0: more keys than that, read again in every pass.
+constexpr int SELECT_BINS = 2048, SELECT_LIST = 256;
+template <int NT, int KPT>
+__global__ __launch_bounds__(NT) void choose_pages_kernel(const SelectParams p) {
+    constexpr int NWV = NT / 64, BPT = SELECT_BINS / NT;
+    __shared__ uint32_t bins[SELECT_BINS];
+    __shared__ uint32_t lkey[SELECT_LIST];
+    __shared__ int lidx[SELECT_LIST], lcount, pick[3];
+    __shared__ uint32_t wred[2][NWV];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int item = blockIdx.x, h = blockIdx.y;
+    const SelectRow r = p.rows[row_of(p, SELECT_MAX_REQS, item, [](const SelectRow& x) { return x.item0; })];
+    const int grp = item - r.item0, tok0 = grp * p.g, m = min(p.g, r.L - tok0);
+    const int lp0 = (r.C + tok0) >> p.logP, lp1 = (r.C + tok0 + m - 1) >> p.logP;
+    const int nfirst = min(p.first, lp1 + 1), cbeg = nfirst, cend = max(cbeg, lp0 - p.last + 1), ntail = lp1 + 1 - cend;
+    const int n = cend - cbeg, need = min(n, p.budget - nfirst - ntail);
+    int32_t* out = p.selected + ((int64_t)(r.out0 + grp) * p.Hkv + h) * p.budget;
+    const int total = nfirst + need + ntail;
+    for (int i = tid; i < p.budget; i += NT) {
+        if (i < nfirst) out[i] = i;
+        else if (i >= nfirst + need) out[i] = i < total ? cend + i - nfirst - need : -1;
+        else if (need == n) out[i] = cbeg + i - nfirst;
+    }
+    if (need == n || need == 0) return;               // nothing to choose (uniform)
+    const int64_t stride = (((int64_t)r.C + r.L + p.P - 1) / p.P + 63) / 64 * 64;
+    const uint32_t* keys = p.keys + (int64_t)r.key0 * 64 + ((int64_t)grp * p.Hkv + h) * stride + cbeg;
+    const int per = KPT ? KPT : (n + NT - 1) / NT;
+    const int i0 = tid * per;
+    uint32_t reg[KPT ? KPT : 1];
+    if constexpr (KPT > 0) {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) reg[i] = i0 + i < n ? keys[i0 + i] : 0u;
+    }
+    // f(key, index) for this thread's keys
+    auto each = [&](auto&& f) {
+        if constexpr (KPT > 0) {
+#pragma unroll
+            for (int i = 0; i < KPT; ++i)
+                if (i0 + i < n) f(reg[i], i0 + i);
+        } else {
+            for (int i = i0; i < min(n, i0 + per); ++i) f(keys[i], i);
+        }
+    };
+    // range of the keys
+    uint32_t lo = 0xffffffffu, hi = 0;
+    each([&](uint32_t k, int) {
+        lo = min(lo, k);
+        hi = max(hi, k);
+    });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+    }
+    if (lane == 0) {
+        wred[0][wave] = lo;
+        wred[1][wave] = hi;
+    }
+    __syncthreads();
+    lo = wred[0][0];
+    hi = wred[1][0];
+    for (int w = 1; w < NWV; ++w) {
+        lo = min(lo, wred[0][w]);
+        hi = max(hi, wred[1][w]);
+    }
+    // keys in (hi, ...] are chosen; of those in [lo, hi] `left` are; the rest is not
+    int left = need;
+    bool all = false;                                 // all of [lo, hi] is chosen
+    bool by_list = false;
+    for (int round = 0; round < 3; ++round) {         // (a range of 32 bits: 21, 10 and 0 are left)
+        const uint32_t range = hi - lo;
+        const int bits = 32 - __clz((int)range);      // (range 0: clz gives 32)
+        const int shift = max(0, bits - 11);
+        for (int i = tid; i < SELECT_BINS; i += NT) bins[i] = 0;
+        __syncthreads();
+        each([&](uint32_t k, int) {
+            if (k >= lo && k <= hi) atomicAdd(&bins[(k - lo) >> shift], 1u);
+        });
+        __syncthreads();
+        // the bin whose keys and those above it reach `left`: bins from the top, BPT per thread
+        uint32_t mine = 0;
+#pragma unroll
+        for (int b = 0; b < BPT; ++b) mine += bins[SELECT_BINS - 1 - (tid * BPT + b)];
+        uint32_t incl = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t v = __shfl_up(incl, o, 64);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 63) wred[0][wave] = incl;
+        __syncthreads();
+        uint32_t before = incl - mine;
+        for (int w = 0; w < wave; ++w) before += wred[0][w];
+        if (before < (uint32_t)left && before + mine >= (uint32_t)left) {
+            uint32_t above = before;
+            for (int b = 0; b < BPT; ++b) {
+                const int bin = SELECT_BINS - 1 - (tid * BPT + b);
+                if (above + bins[bin] >= (uint32_t)left) {
+                    pick[0] = bin;
+                    pick[1] = (int)above;
+                    pick[2] = (int)bins[bin];
+                    break;
+                }
+                above += bins[bin];
+            }
+            lcount = 0;
+        }
+        __syncthreads();
+        const int bin = pick[0], inside = pick[2];
+        left -= pick[1];
+        lo += (uint32_t)bin << shift;
+        hi = min(hi, lo + ((1u << shift) - 1));
+        if (inside == left) {
+            all = true;
+            break;
+        }
+        if (inside <= SELECT_LIST) {
+            by_list = true;
+            break;
+        }
+        if (shift == 0) break;                        // many equal keys: the first `left` of them
+        __syncthreads();
+    }
+    if (by_list) {
+        each([&](uint32_t k, int i) {
+            if (k >= lo && k <= hi) {
+                const int s = atomicAdd(&lcount, 1);
+                lkey[s] = k;
+                lidx[s] = i;
+            }
+        });
+        __syncthreads();
+    }
+    const int inside = pick[2];
+    // how many of this thread's keys are chosen, and of those equal to the border how many it has
+    int count = 0, equal = 0;
+    auto rank_ok = [&](uint32_t k, int i) {           // fewer than `left` of the listed keys come before it
+        int rank = 0;
+        for (int s = 0; s < inside; ++s) rank += lkey[s] > k || (lkey[s] == k && lidx[s] < i) ? 1 : 0;
+        return rank < left;
+    };
+    uint64_t chosen = 0;                              // of this thread's keys (KPT > 0: all fit)
+    each([&](uint32_t k, int i) {
+        bool take = k > hi;
+        if (!take && k >= lo) take = all || (by_list ? rank_ok(k, i) : false);
+        if (!all && !by_list && k >= lo && k <= hi) ++equal;
+        count += take ? 1 : 0;
+        if constexpr (KPT > 0) chosen |= (uint64_t)take << (i - i0);
+    });
+    // exclusive prefixes over the threads
+    auto prefix = [&](int v) {
+        int incl = v;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(incl, o, 64);
+            if (lane >= o) incl += x;
+        }
+        __syncthreads();
+        if (lane == 63) wred[0][wave] = (uint32_t)incl;
+        __syncthreads();
+        int b = incl - v;
+        for (int w = 0; w < wave; ++w) b += (int)wred[0][w];
+        return b;
+    };
+    int eq_before = 0;
+    if (!all && !by_list) {
+        eq_before = prefix(equal);
+        count += min(max(left - eq_before, 0), equal);
+    }
+    int at = nfirst + prefix(count);
+    each([&](uint32_t k, int i) {
+        bool take;
+        if constexpr (KPT > 0) {
+            take = chosen >> (i - i0) & 1;
+        } else {
+            take = k > hi;
+            if (!take && k >= lo) take = all || (by_list ? rank_ok(k, i) : false);
+        }
+        if (!all && !by_list && k >= lo && k <= hi) take = eq_before++ < left;
+        if (take) out[at++] = cbeg + i;
+    });
+}
+
+// ---------------------------------------------------------------------------------------------
+// attention over listed pages
+
+// K/V loader of one wave: blocks of 32 keys, two halves of 16 consecutive slots of a page each (global -> registers -> the wave's LDS region).
+// A block's position in the list decides its page; the list entries of the wave's next 8 blocks come with one load, their page ids with
+// another that is made a block later, so that neither is waited for.
+template <int D, int KVT>
+struct ListLoader {
+    using G_ = Geo<D>;
+    using T = LanePlace<D, KVT, 1>;
+    static constexpr int ES = T::ES;
+    static constexpr int KPL = 1024 / (D * ES);       // keys per load
+    static constexpr int LPH = 16 / KPL;              // loads per half block
+    static constexpr int NL = 2 * LPH;
+    static constexpr int IDS = 8;
+    RawChunk<KVT> k[NL], v[NL];
+    int entry, page;                                  // lane 2 n + h: list entry (-1: none) and page (-1: none) of half h of block n of eight
+    int next;                                         // entries of the eight blocks that follow
+    int first[2];                                     // of the block that was fetched last: position of each half's first key (NONE: no page)
+    int at[2];                                        // ... of the block that is committed
+    float scale[4], sc[4];
+    static constexpr int NONE = 0x3fffffff;
+
+    __device__ __forceinline__ void fetch_entries(const SparseParams& p, const int32_t* list, int last_page, int key0, int step, int end, int j, int lane) {
+        const int pos = key0 + (j + (lane >> 1) % IDS) * step + (lane & 1) * 16;
+        int e = -1;
+        if (pos < end) e = list[pos >> p.logP];
+        next = e <= last_page ? e : -1;
+    }
+    __device__ __forceinline__ void fetch_pages(const SparseParams& p, const int32_t* bt) {
+        entry = next;
+        int id = -1;
+        if (entry >= 0) id = bt[entry];
+        page = (uint32_t)id < (uint64_t)p.num_pages ? id : -1;
+    }
+    // Block j of the wave (the j-th of its eight); false: neither half has a page, and nothing is fetched.
+    __device__ __forceinline__ bool fetch(const SparseParams& p, int kvh, int pos, int j, int lane) {
+        int64_t off[2];
+        int id[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            id[h] = __builtin_amdgcn_readlane(page, 2 * (j % IDS) + h);
+            const int slot = (pos + 16 * h) & (p.P - 1);
+            first[h] = id[h] < 0 ? NONE : (__builtin_amdgcn_readlane(entry, 2 * (j % IDS) + h) << p.logP) + slot;
+            off[h] = slot * (D * ES);
+        }
+        if (id[0] < 0 && id[1] < 0) return false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int use = id[h] < 0 ? id[1 - h] : id[h];        // (a half without a page: any slots of the other's, not used)
+            const int64_t ph = (int64_t)use * p.Hkv + kvh;
+            if constexpr (KVT == KV_FP8) {
+                scale[h] = p.k_scale[ph];
+                scale[2 + h] = p.v_scale[ph];
+            }
+            off[h] += (ph << p.logP) * (D * ES);
+        }
+        uint32_t lo = T::lane_off(lane);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const GlobalBytes ka = scalar_base(static_cast<const char*>(p.k_pool) + off[h]), va = scalar_base(static_cast<const char*>(p.v_pool) + off[h]);
+            asm("" : "+v"(lo));
+#pragma unroll
+            for (int i = 0; i < LPH; ++i) {
+                k[h * LPH + i].v = *(GlobalChunk)(ka + i * 1024 + lo);
+                v[h * LPH + i].v = *(GlobalChunk)(va + i * 1024 + lo);
+            }
+        }
+        return true;
+    }
+    // To LDS; V rows that no row of the item sees become zeros, so that 0-weights never meet NaN garbage (K's logits are replaced).
+    __device__ __forceinline__ void commit(uint32_t kl, uint32_t vl, int last_lim, int lane) {
+#pragma unroll
+        for (int l = 0; l < 4; ++l) sc[l] = KVT == KV_FP8 ? scale[l] : 1.0f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            at[h] = first[h];
+            if (at[h] + 15 > last_lim) {              // uniform
+#pragma unroll
+                for (int i = 0; i < LPH; ++i)
+                    if (at[h] + i * KPL + T::lane_key(lane) > last_lim) v[h * LPH + i].zero();
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            T::put(k[n], sc[n / LPH], kl + T::slot_of(0, lane) + n * (T::GPP * G_::GS));
+            T::put(v[n], sc[2 + n / LPH], vl + T::slot_of(0, lane) + n * (T::GPP * G_::GS));
+        }
+    }
+};
+
+// What an item of sparse attention is about.
+struct SparseItem {
+    int kvh, G, rows;                                 // rows of this tile: row r is row r0 + r of the group, token / G
+    int r0, tok0, C, row_off;
+    int piece, linear;
+    int64_t group;                                    // of the launch
+    int req;
+};
+__device__ __forceinline__ bool sparse_item(const SparseParams& p, int ROWS, int b, SparseItem& it) {
+    it.linear = b;
+    it.kvh = b % p.Hkv;
+    b /= p.Hkv;
+    it.piece = b % p.splits;
+    b /= p.splits;
+    const int tile = b % p.tiles;
+    b /= p.tiles;
+    it.group = b;
+    const SparseRow r = p.rows[row_of(p, SPARSE_MAX_REQS, b, [](const SparseRow& x) { return x.first; })];
+    it.req = r.req;
+    it.G = p.Hq / p.Hkv;
+    it.tok0 = (b - r.first) * p.g;
+    it.C = r.C;
+    it.row_off = r.row_off;
+    it.r0 = tile * ROWS;
+    it.rows = min(ROWS, min(p.g, r.L - it.tok0) * it.G - it.r0);
+    return it.rows > 0;
+}
+
+template <int D, int NW, int ROWS>
+constexpr int sparse_smem() {
+    const int stage = NW * 2 * Geo<D>::B32, merge = NW * ROWS * (D + 4) * 4 + NW * ROWS * 8;
+    return stage > merge ? stage : merge;
+}
+
+// An item: the rows of a group (tokens x heads of a KV head, ROWS at a time) over a piece of the group's list.  The waves take the piece's
+// blocks of 32 keys in turn, each with a softmax state and an LDS region of its own, and the states are merged at the end.
+template <int D, int KVT, int ROWS, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparseParams p) {
+    using G_ = Geo<D>;
+    constexpr bool R16 = ROWS == 16;
+    __shared__ __attribute__((aligned(16))) char smem_raw[sparse_smem<D, NW, ROWS>()];
+    const uint32_t smem = (uint32_t)(uintptr_t)LDS_PTR(char, smem_raw);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    SparseItem it;
+    if (!sparse_item(p, ROWS, blockIdx.x, it)) return;
+    const int row = lane & (ROWS - 1);
+    const bool valid = row < it.rows;
+    const int gr = it.r0 + min(row, it.rows - 1), tok = it.tok0 + gr / it.G;
+    const int lim = it.C + tok;                                           // last visible position
+    const int first_lim = it.C + it.tok0 + it.r0 / it.G, last_lim = it.C + it.tok0 + (it.r0 + it.rows - 1) / it.G;
+    const int last_page = last_lim >> p.logP;
+    const int begin = it.piece * p.chunk, end = min(p.budget << p.logP, begin + p.chunk);
+    const int nblocks = (end - begin + 31) >> 5, step = 32 * NW, key0 = begin + wave * 32;
+    const int nj = (nblocks - wave + NW - 1) / NW;
+    const int32_t* list = p.selected + (it.group * p.Hkv + it.kvh) * p.budget;
+    const int32_t* bt = p.block_table + (int64_t)it.req * p.max_pages;
+
+    ListLoader<D, KVT> ld;
+    if (nj > 0) ld.fetch_entries(p, list, last_page, key0, step, end, 0, lane);
+    bf16x8 Q[R16 ? D / 32 : G_::NKK];
+    {
+        const int hq = it.kvh * it.G + gr % it.G, g = lane / ROWS;
+        const char* src = static_cast<const char*>(p.q) + (((int64_t)(it.row_off + tok) * p.Hq + hq) * D + g * 8) * 2;
+#pragma unroll
+        for (int kk = 0; kk < (R16 ? D / 32 : G_::NKK); ++kk)
+            Q[kk] = __builtin_bit_cast(bf16x8, valid ? *reinterpret_cast<const u32x4*>(src + kk * (R16 ? 64 : 32)) : u32x4{0, 0, 0, 0});
+    }
+    std::conditional_t<R16, WaveAcc16<D>, WaveAcc<D>> st;
+    if constexpr (R16) {
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) st.O[dt] = f32x4{0, 0, 0, 0};
+    } else {
+#pragma unroll
+        for (int db = 0; db < G_::NDB; ++db) st.O[db] = f32x16{0};
+    }
+    st.m = NEG_INF;
+    st.l = 0.0f;
+
+    const uint32_t kl = smem + wave * (2 * G_::B32), vl = kl + G_::B32;
+    bool have = false;
+    if (nj > 0) {
+        ld.fetch_pages(p, bt);
+        have = ld.fetch(p, it.kvh, key0, 0, lane);
+    }
+    for (int j = 0; j < nj; ++j) {
+        const bool now = have;                                            // uniform
+        if (now) ld.commit(kl, vl, last_lim, lane);
+        if (j + 1 < nj) {
+            if ((j + 1) % ld.IDS == 0) ld.fetch_pages(p, bt);
+            have = ld.fetch(p, it.kvh, key0 + (j + 1) * step, j + 1, lane);
+            if ((j + 1) % ld.IDS == ld.IDS - 1) ld.fetch_entries(p, list, last_page, key0, step, end, j + 2, lane);
+        }
+        if (!now) continue;
+        const bool masked = max(ld.at[0], ld.at[1]) + 15 > first_lim;
+        const int sub = R16 ? 4 * key_group16(lane >> 4) : 4 * (lane >> 5);
+        const int rel0 = lim - ld.at[0] - sub, rel1 = lim - ld.at[1] - sub;
+        if constexpr (R16) {
+            f32x4 S[2];
+            qk16<D>(kl, Q, S, lane);
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    S[0][i] = i <= rel0 ? S[0][i] : NEG_INF;
+                    S[1][i] = i <= rel1 ? S[1][i] : NEG_INF;
+                }
+            }
+            float mx = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
+            mx = max_xor32(max_xor16(mx)) * p.c_log2;
+            if (__any(mx > st.m + RESCALE_SLACK)) raise_reference16<D>(st, mx);
+            bf16x8 P;
+            st.l += exp_sum<8>(p.c_log2, st.m == NEG_INF ? 0.0f : st.m, false, [&](int i) { return S[i >> 2][i & 3]; }, [&](int i, __bf16 v) { P[i] = v; });
+            pv16<D>(vl, P, st, lane);
+        } else {
+            f32x16 S;
+            bf16x8 P[2];
+            qk32<D>(kl, Q, S, lane);
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int koff = ((i >> 2) & 1) * 8 + (i & 3);
+                    S[i] = koff <= (i < 8 ? rel0 : rel1) ? S[i] : NEG_INF;
+                }
+            }
+            const float mx = rowmax32(S) * p.c_log2;
+            if (__any(mx > st.m + RESCALE_SLACK)) raise_reference<D>(st, mx);
+            st.l += exp_sum<16>(p.c_log2, st.m == NEG_INF ? 0.0f : st.m, false, [&](int i) { return S[i]; }, [&](int i, __bf16 v) { P[i >> 3][i & 7] = v; });
+            pv32<D>(vl, P, st, lane);
+        }
+    }
+    // merge the waves' states: LDS holds O as [state][row][D + 4] fp32 and (m, l) as [state][row][2]
+    __syncthreads();                                      // every wave is done with its K/V region
+    constexpr int OSTR = D + 4;
+    const uint32_t mlbase = smem + NW * ROWS * OSTR * 4;
+    {
+        const int g = lane / ROWS, slot = wave * ROWS + row;
+        const uint32_t orow = smem + slot * OSTR * 4;
+        const float ltot = R16 ? sum_xor32(sum_xor16(st.l)) : sum_xor32(st.l);
+        if constexpr (R16) {
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) *LDS_PTR(f32x4, orow + (dt * 16 + g * 4) * 4) = st.O[dt];
+        } else {
+#pragma unroll
+            for (int db = 0; db < G_::NDB; ++db)
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    f32x4 o = {st.O[db][i4 * 4], st.O[db][i4 * 4 + 1], st.O[db][i4 * 4 + 2], st.O[db][i4 * 4 + 3]};
+                    *LDS_PTR(f32x4, orow + (db * 32 + i4 * 8 + g * 4) * 4) = o;
+                }
+        }
+        if (g == 0) {
+            *LDS_PTR(float, mlbase + slot * 8) = st.m;
+            *LDS_PTR(float, mlbase + slot * 8 + 4) = ltot;
+        }
+    }
+    __syncthreads();
+    // thread -> (row r, DPT consecutive d): 16 threads per row
+    constexpr int DPT = D / 16;
+    const int dc = (tid & 15) * DPT;
+    for (int r = tid >> 4; r < it.rows; r += 4 * NW) {
+        float mw[NW], lw[NW], mall = NEG_INF;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            mw[w] = *LDS_PTR(float, mlbase + (w * ROWS + r) * 8);
+            lw[w] = *LDS_PTR(float, mlbase + (w * ROWS + r) * 8 + 4);
+            mall = fmaxf(mall, mw[w]);
+        }
+        const float muse = mall == NEG_INF ? 0.0f : mall;
+        float lsum = 0.0f, acc[DPT];
+#pragma unroll
+        for (int x = 0; x < DPT; ++x) acc[x] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float wgt = fast_exp2(mw[w] - muse);
+            lsum += lw[w] * wgt;
+            const uint32_t src = smem + ((w * ROWS + r) * OSTR + dc) * 4;
+#pragma unroll
+            for (int x = 0; x < DPT; x += 4) {
+                const f32x4 o = *LDS_PTR(f32x4, src + x * 4);
+                acc[x] += o[0] * wgt;
+                acc[x + 1] += o[1] * wgt;
+                acc[x + 2] += o[2] * wgt;
+                acc[x + 3] += o[3] * wgt;
+            }
+        }
+        if (p.splits == 1) {
+            const float inv = lsum > 0.0f ? 1.0f / lsum : 0.0f;           // a row that sees no key: zeros
+            const int t = (it.r0 + r) / it.G, hq = it.kvh * it.G + (it.r0 + r) - t * it.G;
+            char* dst = static_cast<char*>(p.out) + (((int64_t)(it.row_off + it.tok0 + t) * p.Hq + hq) * D + dc) * 2;
+#pragma unroll
+            for (int x = 0; x < DPT; x += 4) {
+                bf16x4 o = {(__bf16)(acc[x] * inv), (__bf16)(acc[x + 1] * inv), (__bf16)(acc[x + 2] * inv), (__bf16)(acc[x + 3] * inv)};
+                *reinterpret_cast<u32x2*>(dst + x * 2) = __builtin_bit_cast(u32x2, o);
+            }
+        } else {
+            float* po = p.partial + (int64_t)it.linear * (ROWS * (D + 2)) + r * D + dc;
+#pragma unroll
+            for (int x = 0; x < DPT; x += 4) *reinterpret_cast<f32x4*>(po + x) = f32x4{acc[x], acc[x + 1], acc[x + 2], acc[x + 3]};
+            if ((tid & 15) == 0) {
+                float* ml = p.partial + (int64_t)it.linear * (ROWS * (D + 2)) + ROWS * D + r * 2;
+                ml[0] = mall;
+                ml[1] = lsum;
+            }
+        }
+    }
+}
+
+// Merge the pieces of a list: one workgroup per (group, row tile, KV head) and pass of WG / (D / 4) rows.
+template <int D, int ROWS>
+__global__ __launch_bounds__(WG) void sparse_join_kernel(const SparseParams p) {
+    constexpr int QPR = D / 4, RPP = WG / QPR;
+    SparseItem it;
+    const int b = blockIdx.x, kvh = b % p.Hkv;
+    if (!sparse_item(p, ROWS, (b / p.Hkv) * p.splits * p.Hkv + kvh, it)) return;
+    const int r = blockIdx.y * RPP + threadIdx.x / QPR, dq = (threadIdx.x % QPR) * 4;
+    if (r >= it.rows) return;
+    const int64_t stride = (int64_t)p.Hkv * (ROWS * (D + 2));             // from piece to piece
+    const float* base = p.partial + (int64_t)it.linear * (ROWS * (D + 2));
+    float m = NEG_INF, l = 0.0f;
+    f32x4 acc = {0, 0, 0, 0};
+    constexpr int UN = 8;
+    for (int s0 = 0; s0 < p.splits; s0 += UN) {
+        float mv[UN], lv[UN];
+        f32x4 ov[UN];
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const float* part = base + min(s0 + i, p.splits - 1) * stride;
+            mv[i] = part[ROWS * D + r * 2];
+            lv[i] = part[ROWS * D + r * 2 + 1];
+            ov[i] = *reinterpret_cast<const f32x4*>(part + r * D + dq);
+        }
+        float mg = m;
+#pragma unroll
+        for (int i = 0; i < UN; ++i) mg = fmaxf(mg, mv[i]);
+        const float muse = mg == NEG_INF ? 0.0f : mg, back = fast_exp2(m - muse);
+        l *= back;
+        acc *= back;
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            if (s0 + i < p.splits) {
+                const float w = fast_exp2(mv[i] - muse);
+                l += lv[i] * w;
+                acc += ov[i] * w;
+            }
+        }
+        m = mg;
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const int t = (it.r0 + r) / it.G, hq = it.kvh * it.G + (it.r0 + r) - t * it.G;
+    char* dst = static_cast<char*>(p.out) + (((int64_t)(it.row_off + it.tok0 + t) * p.Hq + hq) * D + dq) * 2;
+    bf16x4 o = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
+    *reinterpret_cast<u32x2*>(dst) = __builtin_bit_cast(u32x2, o);
+}
+
+// ---------------------------------------------------------------------------------------------
+// launchers
+
+constexpr int64_t MAX_PAGES = 1 << 22;                // pages per launch (a grid holds fewer than 2^32 threads)
+
+template <int D, int P, int KVT>
+static void rope_t(const RopeParams& p, unsigned nx, unsigned ny, hipStream_t st) {
+    if (p.codes)
+        hipLaunchKernelGGL((rope_append_kernel<D, P, KVT, true>), dim3(nx, ny), dim3(WG), 0, st, p);
+    else
+        hipLaunchKernelGGL((rope_append_kernel<D, P, KVT, false>), dim3(nx, ny), dim3(WG), 0, st, p);
+}
+template <int D, int KVT>
+static void rope_p(const RopeParams& p, unsigned nx, unsigned ny, hipStream_t st) {
+    if (p.a.P == 16) rope_t<D, 16, KVT>(p, nx, ny, st);
+    else if (p.a.P == 32) rope_t<D, 32, KVT>(p, nx, ny, st);
+    else rope_t<D, 64, KVT>(p, nx, ny, st);
+}
+
+// max_new: the most new tokens of a page
+hipError_t launch_rope(RopeParams& p, int kvt, int64_t pages, int max_new, hipStream_t st) {
+    const int64_t jobs = 2 * p.a.Hkv + (p.q ? ((int64_t)max_new * p.Hq * (p.a.D / 16) + 255) / 256 : 0);
+    // a wave per job while that fills the chip; in long launches the waves of a page share its jobs, and its angles, among fewer
+    const int64_t ny = std::min((jobs + 3) / 4, std::max<int64_t>(1, 2048 / pages));
+    for (int64_t at = 0; at < pages; at += MAX_PAGES) {
+        p.a.pg0 = (int32_t)at;
+        const unsigned nx = (unsigned)std::min(MAX_PAGES, pages - at);
+        if (p.a.D == 128) {
+            if (kvt == KV_BF16) rope_p<128, KV_BF16>(p, nx, (unsigned)ny, st);
+            else rope_p<128, KV_FP8>(p, nx, (unsigned)ny, st);
+        } else {
+            if (kvt == KV_BF16) rope_p<64, KV_BF16>(p, nx, (unsigned)ny, st);
+            else rope_p<64, KV_FP8>(p, nx, (unsigned)ny, st);
+        }
+    }
+    return hipGetLastError();
+}
+
+template <int D, int KVT>
+static void bounds_p(const BoundsParams& p, dim3 grid, hipStream_t st) {
+    if (p.a.P == 16) hipLaunchKernelGGL((page_bounds_kernel<D, 16, KVT>), grid, dim3(WG), 0, st, p);
+    else if (p.a.P == 32) hipLaunchKernelGGL((page_bounds_kernel<D, 32, KVT>), grid, dim3(WG), 0, st, p);
+    else hipLaunchKernelGGL((page_bounds_kernel<D, 64, KVT>), grid, dim3(WG), 0, st, p);
+}
+
+hipError_t launch_bounds(BoundsParams& p, int kvt, int64_t pages, hipStream_t st) {
+    for (int64_t at = 0; at < pages; at += MAX_PAGES) {
+        p.a.pg0 = (int32_t)at;
+        const dim3 grid((unsigned)std::min(MAX_PAGES, pages - at), (p.a.Hkv + 3) / 4);
+        if (p.a.D == 128) {
+            if (kvt == KV_BF16) bounds_p<128, KV_BF16>(p, grid, st);
+            else bounds_p<128, KV_FP8>(p, grid, st);
+        } else {
+            if (kvt == KV_BF16) bounds_p<64, KV_BF16>(p, grid, st);
+            else bounds_p<64, KV_FP8>(p, grid, st);
+        }
+    }
+    return hipGetLastError();
+}
+
+template <int D>
+static void select_t(const SelectParams& p, int groups, int score_blocks, int64_t max_keys, hipStream_t st) {
+    bool one = true;
+    for (int i = 0; i < p.n; ++i) one &= p.rows[i].L <= p.g;
+    if (score_blocks > 0) {
+        const int heads = score_heads(p.Hkv);
+        const dim3 grid(score_blocks, (p.Hkv + heads - 1) / heads);
+        if (one) {
+            hipLaunchKernelGGL((page_scores_kernel<D, true>), grid, dim3(64 * SCORE_WAVES), 0, st, p, heads);
+        } else {
+            hipLaunchKernelGGL((query_codes_kernel<D>), dim3(groups, p.Hkv), dim3(64), 0, st, p);
+            hipLaunchKernelGGL((page_scores_kernel<D, false>), grid, dim3(64 * SCORE_WAVES), 0, st, p, heads);
+        }
+    }
+    const dim3 grid(groups, p.Hkv);
+    if (max_keys <= 256 * 4) hipLaunchKernelGGL((choose_pages_kernel<256, 4>), grid, dim3(256), 0, st, p);
+    else if (max_keys <= 256 * 16) hipLaunchKernelGGL((choose_pages_kernel<256, 16>), grid, dim3(256), 0, st, p);
+    else if (max_keys <= 1024 * 16) hipLaunchKernelGGL((choose_pages_kernel<1024, 16>), grid, dim3(1024), 0, st, p);
+    else hipLaunchKernelGGL((choose_pages_kernel<1024, 0>), grid, dim3(1024), 0, st, p);
+}
+
+// groups: of this launch; score_blocks: workgroup columns of the score launch (0: every group takes all its pages); max_keys: the most pages
+// a group chooses from
+hipError_t launch_select(const SelectParams& p, int D, int groups, int score_blocks, int64_t max_keys, hipStream_t st) {
+    if (D == 128) select_t<128>(p, groups, score_blocks, max_keys, st);
+    else select_t<64>(p, groups, score_blocks, max_keys, st);
+    return hipGetLastError();
+}
+
+template <int D, int KVT>
+static void sparse_t(const SparseParams& p, int groups, hipStream_t st) {
+    const int64_t items = (int64_t)groups * p.tiles * p.Hkv;
+    const dim3 grid((unsigned)(items * p.splits)), join((unsigned)items, 1);
+    if (sparse_tile(p.g * (p.Hq / p.Hkv)) == 16) {
+        hipLaunchKernelGGL((sparse_rows_kernel<D, KVT, 16, 4>), grid, dim3(256), 0, st, p);
+        if (p.splits > 1) hipLaunchKernelGGL((sparse_join_kernel<D, 16>), dim3((unsigned)items, 16 * D / 4 / WG), dim3(WG), 0, st, p);
+    } else {
+        hipLaunchKernelGGL((sparse_rows_kernel<D, KVT, 32, 4>), grid, dim3(256), 0, st, p);
+        if (p.splits > 1) hipLaunchKernelGGL((sparse_join_kernel<D, 32>), dim3((unsigned)items, 32 * D / 4 / WG), dim3(WG), 0, st, p);
+    }
+}
+
+hipError_t launch_sparse(const SparseParams& p, int D, int kvt, int groups, hipStream_t st) {
+    if (D == 128) {
+        if (kvt == KV_BF16) sparse_t<128, KV_BF16>(p, groups, st);
+        else sparse_t<128, KV_FP8>(p, groups, st);
+    } else {
+        if (kvt == KV_BF16) sparse_t<64, KV_BF16>(p, groups, st);
+        else sparse_t<64, KV_FP8>(p, groups, st);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace ampd

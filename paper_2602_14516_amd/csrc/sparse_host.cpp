@@ -1,0 +1,196 @@
+// Sparse attention, host half: argument validation, how a call is cut into launches, workspace sizes.  Nothing here includes or calls HIP.
+#include "sparse.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "api_host.h"
+
+namespace ampd {
+namespace host {
+
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+ampd_status validate_rope(const ampd_kv_cache* c, const ampd_batch* b, const ampd_rope* rope, const ampd_qkv_rows* rows, const void* q_out) {
+    const ampd_status vs = validate(c, b, true);
+    if (vs != AMPD_OK) return vs;
+    if (!rope || !rows || rope->reserved != 0) return AMPD_ERR_INVALID_ARG;
+    if (rope->interleaved != 0 && rope->interleaved != 1) return AMPD_ERR_INVALID_ARG;
+    if (!(rope->scale > 0.0f) || !std::isfinite(rope->scale)) return AMPD_ERR_INVALID_ARG;
+    if (rope->rotary_dim < 16 || rope->rotary_dim > c->head_dim || rope->rotary_dim % 16 != 0) return AMPD_ERR_UNSUPPORTED;
+    int64_t sumL = 0;
+    for (int r = 0; r < b->num_reqs; ++r) sumL += b->h_incr_len[r];
+    if (sumL == 0) return AMPD_OK;
+    if (!rope->inv_freq || !rows->k || !rows->v || (rows->q && !q_out)) return AMPD_ERR_INVALID_ARG;
+    const int64_t q_row = (int64_t)c->num_q_heads * c->head_dim, kv_row = (int64_t)c->num_kv_heads * c->head_dim;
+    const struct {
+        const void* p;
+        int64_t stride, row;
+    } in[3] = {{rows->k, rows->k_stride, kv_row}, {rows->v, rows->v_stride, kv_row}, {rows->q, rows->q_stride, q_row}};
+    for (const auto& x : in) {
+        if (!x.p) continue;
+        if (!aligned16(x.p) || x.stride < x.row || x.stride % 8 != 0 || x.stride > (int64_t)1 << 40) return AMPD_ERR_INVALID_ARG;
+    }
+    if (rows->q && !aligned16(q_out)) return AMPD_ERR_INVALID_ARG;
+    if (rows->q && rows->q == q_out && rows->q_stride != q_row) return AMPD_ERR_INVALID_ARG;
+    return AMPD_OK;
+}
+
+ampd_status validate_bounds(const ampd_page_bounds* bounds) {
+    if (!bounds || !bounds->codes || !bounds->scale || !aligned16(bounds->codes)) return AMPD_ERR_INVALID_ARG;
+    return AMPD_OK;
+}
+
+static ampd_status validate_group(const ampd_kv_cache* c, int32_t budget, int32_t group_tokens) {
+    if (budget < 1 || group_tokens < 1) return AMPD_ERR_INVALID_ARG;
+    if ((int64_t)group_tokens * (c->num_q_heads / c->num_kv_heads) > SPARSE_MAX_ROWS) return AMPD_ERR_UNSUPPORTED;
+    if ((int64_t)budget * c->page_size > (int64_t)1 << 29) return AMPD_ERR_UNSUPPORTED;
+    return AMPD_OK;
+}
+
+ampd_status validate_select(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* s) {
+    ampd_status vs = validate(c, b, false);
+    if (vs != AMPD_OK) return vs;
+    if (!s) return AMPD_ERR_INVALID_ARG;
+    for (int i = 0; i < 4; ++i)
+        if (s->reserved[i] != 0) return AMPD_ERR_INVALID_ARG;
+    vs = validate_group(c, s->budget, s->group_tokens);
+    if (vs != AMPD_OK) return vs;
+    if (s->first_pages < 0 || s->last_pages < 1) return AMPD_ERR_INVALID_ARG;
+    const int64_t always = (int64_t)s->first_pages + s->last_pages + (s->group_tokens - 1 + c->page_size - 1) / c->page_size;
+    return s->budget < always ? AMPD_ERR_INVALID_ARG : AMPD_OK;
+}
+
+ampd_status validate_sparse(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, int32_t group_tokens) {
+    const ampd_status vs = validate(c, b, false);
+    return vs != AMPD_OK ? vs : validate_group(c, budget, group_tokens);
+}
+
+ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* s, LaunchFn<SelectLaunch> f) {
+    const int P = c->page_size, logP = log2_exact(P), g = s->group_tokens, Hkv = c->num_kv_heads;
+    const int64_t most_groups = std::max<int64_t>(1, (1 << 21) / Hkv);        // a grid holds fewer than 2^32 threads
+    SelectLaunch l;
+    ampd_status st = AMPD_OK;
+    auto flush = [&]() {
+        if (l.n > 0 && st == AMPD_OK) st = f(l);
+        l = SelectLaunch();
+    };
+    int64_t row_off = 0, out0 = 0;
+    for (int r = 0; r < b->num_reqs && st == AMPD_OK; ++r) {
+        const int64_t C = b->h_ctx_len[r], L = b->h_incr_len[r], groups = groups_of(L, g);
+        const int64_t per_group = Hkv * key_stride(C + L, P);
+        for (int64_t at = 0; at < groups && st == AMPD_OK;) {
+            if (l.n == SELECT_MAX_REQS || l.groups == most_groups || (l.keys > 0 && l.keys + per_group > SELECT_KEYS)) {
+                flush();
+                if (st != AMPD_OK) break;
+            }
+            const int64_t take = std::min({groups - at, most_groups - l.groups, std::max<int64_t>(1, (SELECT_KEYS - l.keys) / per_group)});
+            SelectRow& x = l.rows[l.n++];
+            x.C = (int32_t)(C + at * g);
+            x.L = (int32_t)std::min(L - at * g, take * g);
+            x.row_off = (int32_t)(row_off + at * g);
+            x.req = r;
+            x.out0 = (int32_t)(out0 + at);
+            x.item0 = l.groups;
+            x.tile0 = l.score_blocks;
+            x.key0 = (uint32_t)(l.keys / 64);
+            l.groups += (int)take;
+            // pages that the last group of these may choose by score (the others: no more)
+            const int64_t tok0 = (take - 1) * g, lp0 = (x.C + tok0) >> logP, lp1 = (x.C + x.L - 1) >> logP, end = lp0 - s->last_pages + 1;
+            if (end > s->first_pages && lp1 + 1 > s->budget) {
+                l.max_keys = std::max(l.max_keys, end - s->first_pages);
+                l.score_blocks += (int)((take + 15) / 16 * ((end + score_pages(Hkv) - 1) / score_pages(Hkv)));
+                l.keys += take * Hkv * key_stride((int64_t)x.C + x.L, P);
+            }
+            at += take;
+        }
+        row_off += L;
+        out0 += groups;
+    }
+    flush();
+    return st;
+}
+
+int64_t select_keys_bytes(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* s) {
+    int64_t most = 0;
+    select_launches(c, b, s, [&](const SelectLaunch& l) {
+        most = std::max(most, l.keys * 4);
+        return AMPD_OK;
+    });
+    return (most + 255) / 256 * 256;
+}
+
+ampd_status sparse_launches(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, int32_t g, LaunchFn<SparseLaunch> f) {
+    const int Hkv = c->num_kv_heads, rows = g * (c->num_q_heads / Hkv), tile = sparse_tile(rows), tiles = (rows + tile - 1) / tile;
+    const int64_t most_groups = std::max<int64_t>(1, (1 << 22) / ((int64_t)Hkv * tiles));     // a grid holds fewer than 2^32 threads
+    const int64_t keys = (int64_t)budget * c->page_size;
+    SparseLaunch l;
+    ampd_status st = AMPD_OK;
+    auto flush = [&](int64_t next) {
+        if (l.n > 0 && st == AMPD_OK) {
+            l.tiles = tiles;
+            // Two workgroups of 4 waves to a CU fill the chip: fewer items are cut into pieces, of a block of 32 keys per wave at least.
+            const int64_t items = (int64_t)l.groups * tiles * Hkv, want = std::max<int64_t>(1, 512 / items), least = 4 * 32;
+            const int64_t per = ((keys + want - 1) / want + least - 1) / least * least;
+            l.chunk = (int)per;
+            l.splits = (int)((keys + per - 1) / per);
+            l.partial_floats = l.splits > 1 ? items * l.splits * tile * (c->head_dim + 2) : 0;
+            st = f(l);
+        }
+        l = SparseLaunch();
+        l.group0 = next;
+    };
+    int64_t row_off = 0, group = 0;
+    for (int r = 0; r < b->num_reqs && st == AMPD_OK; ++r) {
+        const int64_t L = b->h_incr_len[r], groups = groups_of(L, g);
+        for (int64_t at = 0; at < groups && st == AMPD_OK;) {
+            if (l.n == SPARSE_MAX_REQS || l.groups == most_groups) {
+                flush(group + at);
+                if (st != AMPD_OK) break;
+            }
+            const int64_t take = std::min(groups - at, most_groups - l.groups);
+            SparseRow& x = l.rows[l.n++];
+            x.C = (int32_t)(b->h_ctx_len[r] + at * g);
+            x.L = (int32_t)std::min(L - at * g, take * g);
+            x.row_off = (int32_t)(row_off + at * g);
+            x.req = r;
+            x.first = l.groups;
+            l.groups += (int)take;
+            at += take;
+        }
+        row_off += L;
+        group += groups;
+    }
+    flush(group);
+    return st;
+}
+
+}  // namespace host
+}  // namespace ampd
+
+using namespace ampd;
+using namespace ampd::host;
+
+extern "C" {
+
+size_t ampd_select_pages_workspace_bytes(const ampd_kv_cache* cache, const ampd_batch* batch, const ampd_page_selection* sel) {
+    if (validate_select(cache, batch, sel) != AMPD_OK) return 0;
+    int64_t groups = 0;
+    select_launches(cache, batch, sel, [&](const SelectLaunch& l) {
+        groups = std::max(groups, (int64_t)l.groups);
+        return AMPD_OK;
+    });
+    return (size_t)std::max<int64_t>(256, select_keys_bytes(cache, batch, sel) + groups * cache->num_kv_heads * 4 * cache->head_dim);
+}
+
+size_t ampd_sparse_attn_workspace_bytes(const ampd_kv_cache* cache, const ampd_batch* batch, int32_t budget, int32_t group_tokens) {
+    if (validate_sparse(cache, batch, budget, group_tokens) != AMPD_OK) return 0;
+    int64_t floats = 0;
+    sparse_launches(cache, batch, budget, group_tokens, [&](const SparseLaunch& l) {
+        floats = std::max(floats, l.partial_floats);
+        return AMPD_OK;
+    });
+    return (size_t)std::max<int64_t>(256, floats * 4);
+}
+
+}  // extern "C"
