@@ -23,12 +23,18 @@ constexpr int64_t SELECT_KEYS = 16 << 20;
 // Row tile of a sparse-attention workgroup: 16 query rows, or 32 where a group has more.
 inline int sparse_tile(int rows) { return rows <= 16 ? 16 : 32; }
 
-// Pages that a wave of the score launch goes through, 16 at a time; a workgroup's waves are `score_heads` neighbouring heads of the same
-// pages, then neighbouring pages.
-constexpr int SCORE_TILES = 8;
-constexpr int SCORE_WAVES = 8;
-inline int score_heads(int Hkv) { return Hkv >= 8 ? 8 : Hkv > 2 ? 4 : Hkv; }
-inline int score_pages(int Hkv) { return SCORE_TILES * 16 * (SCORE_WAVES / score_heads(Hkv)); }
+// A wave of the score launch goes through score_tiles tiles of 16 pages, SCORE_BATCH at a time; a workgroup's waves are `score_heads`
+// neighbouring heads of the same pages, then neighbouring pages.  Long launches give a wave more tiles, which spares it queries to quantise,
+// until some 3 000 waves are left (96 rows of 2-16 k tokens, 8 KV heads: 2, 4, 8, 12, 16 tiles 35.6, 30.3, 29.0, 30.7, 34.8 us; 4 rows of
+// 36-70 k, one head: 5.4, 6.0, 7.5, 8.6, 10.1).  Batches of 4 tiles and workgroups of 8 waves leave a CU fewer waves: 32.7 us.
+constexpr int SCORE_BATCH = 2;
+constexpr int SCORE_WAVES = 4;
+inline int score_heads(int Hkv) { return Hkv > 2 ? 4 : Hkv; }
+inline int score_pages(int Hkv, int score_tiles) { return score_tiles * 16 * (SCORE_WAVES / score_heads(Hkv)); }
+inline int score_tiles(int64_t tiles) {
+    const int64_t t = tiles / 3072 / SCORE_BATCH * SCORE_BATCH;
+    return (int)(t < SCORE_BATCH ? SCORE_BATCH : t > 64 ? 64 : t);
+}
 
 // ---- launches ----------------------------------------------------------------------------------
 // The rows of a launch travel as kernel arguments.  A row with more groups than one launch takes is handed on as a row whose context begins
@@ -43,7 +49,7 @@ struct SelectRow {
     uint32_t key0;            // the row's first key in the workspace, in units of 64 keys
 };
 struct SelectLaunch {
-    int n = 0, groups = 0, score_blocks = 0;
+    int n = 0, groups = 0, score_blocks = 0, score_tiles = 0;
     int64_t keys = 0;         // in the workspace
     int64_t max_keys = 0;     // the most pages that a group chooses from
     SelectRow rows[SELECT_MAX_REQS];
@@ -57,7 +63,8 @@ struct SparseRow {
 struct SparseLaunch {
     int n = 0, groups = 0;
     int64_t group0 = 0;       // number of its first group in the batch
-    int tiles = 1, splits = 1, chunk = 0;     // row tiles of a group; pieces of a list; keys per piece (a multiple of 32)
+    int tiles = 1, waves = 4;  // row tiles of a group; waves of a workgroup
+    int splits = 1, chunk = 0; // pieces of a list; keys per piece (a multiple of 32)
     int64_t partial_floats = 0;
     SparseRow rows[SPARSE_MAX_REQS];
 };
@@ -133,7 +140,7 @@ struct SelectParams {
     int64_t num_pages;
     int32_t Hq, Hkv, P, logP, max_pages;
     int32_t budget, first, last, g;
-    int32_t n;
+    int32_t score_tiles, n;
     SelectRow rows[SELECT_MAX_REQS];
 };
 
@@ -158,7 +165,7 @@ struct SparseParams {
 hipError_t launch_rope(RopeParams& p, int kvt, int64_t pages, int max_new, hipStream_t st);
 hipError_t launch_bounds(BoundsParams& p, int kvt, int64_t pages, hipStream_t st);
 hipError_t launch_select(const SelectParams& p, int D, int groups, int score_blocks, int64_t max_keys, hipStream_t st);
-hipError_t launch_sparse(const SparseParams& p, int D, int kvt, int groups, hipStream_t st);
+hipError_t launch_sparse(const SparseParams& p, int D, int kvt, int groups, int waves, hipStream_t st);
 
 }  // namespace ampd
 #endif

@@ -122,7 +122,8 @@ __device__ __forceinline__ void store_bounds(LaneBounds& b, float unit, int ca, 
     if (lane == 0) *scale = __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
-// A wave per page and KV head.
+// A wave per page and KV head.  Non-temporal loads: 165 MB 31.5 us instead of 35.2.  (Two heads per wave 30.6 us, but a reply of 701 tokens 4.7
+// instead of 3.8.)
 template <int D, int P, int KVT>
 __global__ __launch_bounds__(WG) void page_bounds_kernel(const BoundsParams p) {
     constexpr int PPT = Units<D>::PPT, NU = Units<D>::COUNT(P);
@@ -141,10 +142,10 @@ __global__ __launch_bounds__(WG) void page_bounds_kernel(const BoundsParams p) {
     for (int k = 0; k < NU; ++k) {
         const int s = min((lane + 64 * k) / PPT, slots - 1);              // (a slot behind the last token: the last token's once more)
         if constexpr (KVT == KV_BF16) {
-            x[k] = *reinterpret_cast<const u32x4*>(pg + s * (D * 2) + pair * 16);
-            y[k] = *reinterpret_cast<const u32x4*>(pg + s * (D * 2) + (pair + PPT) * 16);
+            x[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pg + s * (D * 2) + pair * 16));
+            y[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pg + s * (D * 2) + (pair + PPT) * 16));
         } else {
-            x[k] = *reinterpret_cast<const u32x4*>(pg + s * D + pair * 16);
+            x[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pg + s * D + pair * 16));
         }
     }
 #pragma unroll
@@ -169,22 +170,25 @@ __global__ __launch_bounds__(WG) void page_bounds_kernel(const BoundsParams p) {
 // ---------------------------------------------------------------------------------------------
 // rotate and append
 
-// The chunks of a pair: while rotated elements remain, two chunks whose elements the rotation pairs (half apart) or two chunks of
-// neighbouring pairs (interleaved); behind them two neighbouring chunks that are copied.
+// The chunks of a pair, so that the lanes of a key take neighbouring chunks with each load: two whose elements the rotation pairs (half
+// apart) or, where it pairs neighbours or copies, any two.  ra, rb: whether they are rotated; a chunk of 8 elements is so as a whole.
 struct ChunkPair {
     int a, b;
-    bool rotated;
+    bool ra, rb;
 };
-__device__ __forceinline__ ChunkPair chunk_pair(int pair, int rd) {
+template <int D>
+__device__ __forceinline__ ChunkPair chunk_pair(int pair, int rd, bool interleaved) {
+    constexpr int PPT = Units<D>::PPT;
     const int half = rd >> 4;
-    if (pair < half) return {pair, pair + half, true};
-    return {2 * pair, 2 * pair + 1, false};           // (rd / 8 + 2 (pair - rd / 16))
+    if (interleaved) return {pair, pair + PPT, pair < 2 * half, pair + PPT < 2 * half};
+    if (pair < half) return {pair, pair + half, true, true};
+    return {half + pair, PPT + pair, false, false};   // (the rest, 2 half .. 2 PPT, in two runs)
 }
 
 // Rotate a pair of chunks in type F; cs(i): cosine and sine of the i-th of the 8 angles of the pair (half apart: those of elements 0..7;
 // interleaved: of the 4 pairs of chunk a, then of chunk b).
 template <class F, class CS>
-__device__ __forceinline__ void rotate(u32x4& va, u32x4& vb, bool interleaved, CS&& cs) {
+__device__ __forceinline__ void rotate(u32x4& va, u32x4& vb, const ChunkPair& cp, bool interleaved, CS&& cs) {
     float a[8], b[8];
     unpack8(va, a);
     unpack8(vb, b);
@@ -199,17 +203,27 @@ __device__ __forceinline__ void rotate(u32x4& va, u32x4& vb, bool interleaved, C
         y2 = (__bf16)f2;
     };
     if (interleaved) {                                // uniform
+        if (cp.ra) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __bf16 y1, y2;
-            turn(i, a[2 * i], a[2 * i + 1], y1, y2);
-            ra[2 * i] = y1;
-            ra[2 * i + 1] = y2;
-            turn(4 + i, b[2 * i], b[2 * i + 1], y1, y2);
-            rb[2 * i] = y1;
-            rb[2 * i + 1] = y2;
+            for (int i = 0; i < 4; ++i) {
+                __bf16 y1, y2;
+                turn(i, a[2 * i], a[2 * i + 1], y1, y2);
+                ra[2 * i] = y1;
+                ra[2 * i + 1] = y2;
+            }
+            va = __builtin_bit_cast(u32x4, ra);
         }
-    } else {
+        if (cp.rb) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                __bf16 y1, y2;
+                turn(4 + i, b[2 * i], b[2 * i + 1], y1, y2);
+                rb[2 * i] = y1;
+                rb[2 * i + 1] = y2;
+            }
+            vb = __builtin_bit_cast(u32x4, rb);
+        }
+    } else if (cp.ra) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             __bf16 y1, y2;
@@ -217,9 +231,9 @@ __device__ __forceinline__ void rotate(u32x4& va, u32x4& vb, bool interleaved, C
             ra[i] = y1;
             rb[i] = y2;
         }
+        va = __builtin_bit_cast(u32x4, ra);
+        vb = __builtin_bit_cast(u32x4, rb);
     }
-    va = __builtin_bit_cast(u32x4, ra);
-    vb = __builtin_bit_cast(u32x4, rb);
 }
 
 // One workgroup column per page that new tokens fall into; the column's waves share its jobs: K of a head, V of a head (the page's new tokens
@@ -247,7 +261,7 @@ __global__ __launch_bounds__(WG) void rope_append_kernel(const RopeParams p) {
     }
     __syncthreads();
     const int nkv = (uint32_t)j.page < (uint64_t)p.num_pages ? 2 * a.Hkv : 0, nq = p.q ? (n * p.Hq * PPT + 255) / 256 : 0;
-    const ChunkPair cp = chunk_pair(lane % PPT, p.rd);
+    const ChunkPair cp = chunk_pair<D>(lane % PPT, p.rd, p.interleaved);
     // the i-th angle of the lane's pair, in table order
     const int f0 = p.interleaved ? 4 * cp.a : 8 * cp.a, f1 = p.interleaved ? 4 * cp.b - 4 : f0;   // angles 0..3 from f0, 4..7 from f1
     for (int job = blockIdx.y * (WG / 64) + wave; job < nkv + nq; job += gridDim.y * (WG / 64)) {
@@ -267,9 +281,9 @@ __global__ __launch_bounds__(WG) void rope_append_kernel(const RopeParams p) {
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (cp.rotated) {
+                if (cp.ra || cp.rb) {
                     const f32x2* t = head + tok[k] * F;
-                    rotate<float>(x[k], y[k], p.interleaved, [&](int i, float& c, float& s) {
+                    rotate<float>(x[k], y[k], cp, p.interleaved, [&](int i, float& c, float& s) {
                         const f32x2 v = t[(i < 4 ? f0 : f1) + i];
                         c = v.x;
                         s = v.y;
@@ -321,13 +335,13 @@ __global__ __launch_bounds__(WG) void rope_append_kernel(const RopeParams p) {
                     }
                 }
             }
-            if (!is_v && cp.rotated) {
+            if (!is_v && (cp.ra || cp.rb)) {
 #pragma unroll
                 for (int k = 0; k < RUN; ++k) {
                     const int s = (base + 64 * k) / PPT;
                     if (s >= s0 && s < s0 + n) {
                         const int t = (s - s0) * F;
-                        rotate<double>(x[k], y[k], p.interleaved, [&](int i, double& c, double& sn) {
+                        rotate<double>(x[k], y[k], cp, p.interleaved, [&](int i, double& c, double& sn) {
                             const f32x2 v = head[t + (i < 4 ? f0 : f1) + i], w = tail[t + (i < 4 ? f0 : f1) + i];
                             c = (double)v.x + (double)w.x;
                             sn = (double)v.y + (double)w.y;
@@ -412,14 +426,25 @@ __global__ __launch_bounds__(WG) void rope_append_kernel(const RopeParams p) {
 // ---------------------------------------------------------------------------------------------
 // page selection
 
-// Which row of a launch owns item idx: the last one that starts at or before it.
-template <class P, class F>
-__device__ __forceinline__ int row_of(const P& p, int max_rows, int idx, F&& start) {
+// The row of a launch that owns item idx: the last one that starts at or before it.  Every lane loads a row or two and the owner's is picked
+// from the lanes: one trip to the arguments.
+template <int MAX, class Row, class F>
+__device__ __forceinline__ Row row_of(const Row* rows, int n, int idx, F&& start) {
+    static_assert(MAX > 64 && MAX <= 128 && sizeof(Row) % 4 == 0, "two rows per lane");
+    constexpr int W = sizeof(Row) / 4;
+    struct Words {
+        int32_t w[W];
+    };
     const int lane = threadIdx.x & 63;
-    int r = -1;
-    for (int base = 0; base < max_rows && base < p.n; base += 64)
-        r += __popcll(__ballot(base + lane < p.n && start(p.rows[min(base + lane, p.n - 1)]) <= idx));
-    return __builtin_amdgcn_readfirstlane(r);
+    const Row a = rows[min(lane, n - 1)];
+    Row b = a;
+    if (n > 64) b = rows[min(lane + 64, n - 1)];
+    const int r = __popcll(__ballot(lane < n && start(a) <= idx)) + __popcll(__ballot(lane + 64 < n && start(b) <= idx)) - 1;
+    const Words x = __builtin_bit_cast(Words, a), y = __builtin_bit_cast(Words, b);
+    Words out;
+#pragma unroll
+    for (int i = 0; i < W; ++i) out.w[i] = __builtin_amdgcn_readlane(r < 64 ? x.w[i] : y.w[i], r & 63);
+    return __builtin_bit_cast(Row, out);
 }
 
 template <int CTRL>
@@ -434,86 +459,221 @@ __device__ __forceinline__ uint32_t row_sum(uint32_t x) {
     return add_dpp<0x128>(x);                         // row_ror:8
 }
 
+__device__ __forceinline__ uint32_t max16x2(uint32_t a, uint32_t b) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
+    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
+    x = max_dpp<0xB1>(x);
+    x = max_dpp<0x4E>(x);
+    x = max_dpp<0x124>(x);
+    x = max_dpp<0x128>(x);
+    u32x2 r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max(r[0], r[1]);
+}
+__device__ __forceinline__ uint32_t wave_umin(uint32_t x) { return ~wave_umax(~x); }
+__device__ __forceinline__ uint32_t wave_usum(uint32_t x) {
+    x = row_sum(x);
+    u32x2 r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = r[0] + r[1];
+    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return r[0] + r[1];
+}
+
+// bytes b < 128 -> -b: 128 - b has bit 7 set where b is 0 alone; with bit 7 flipped it is -b modulo 256
+__device__ __forceinline__ uint32_t negate_bytes(uint32_t x) { return (0x80808080u - x) ^ 0x80808080u; }
+
+// 2^-f for the smallest f with amax <= 127 * 2^f, in two factors: f reaches -133 and 123 (a group of zeros: any)
+__device__ __forceinline__ void query_step(uint32_t amax_bits, float& m0, float& m1) {
+    const int ex = (int)(amax_bits >> 23) - 127, f = (amax_bits & 0x7fffffu) <= 0x7e0000u ? ex - 6 : ex - 5;
+    const int fs = max(-126, min(127, -f));
+    m0 = __uint_as_float((uint32_t)(fs + 127) << 23);
+    m1 = __uint_as_float((uint32_t)(max(-126, min(127, -f - fs)) + 127) << 23);
+}
+
 // Whole numbers of a group's queries for one KV head, summed over its rows (tokens x heads), as two limbs of 7 bits in the operand layout of
 // the 16x16x64 product: lane l holds bytes 16 (l / 16) .. of k-block kk; k = 0..d-1 the sums of the positive parts, d..2d-1 of the
 // negative ones.  Every lane of a row of 16 ends up with the same.  At most 128 rows of at most 127 each: sums below 2^14.
+// The lanes of a row of 16 take the group's rows in turn; start() fetches the first 16, so that other loads can be issued behind them.
 template <int D>
-__device__ __forceinline__ void quantise_queries(const char* q, int64_t token_bytes, int G, int rows, int lane, i32x4 (&limb)[2][D / 32]) {
-    constexpr int NB = D / 64;                        // 64-channel blocks
-    const int col = lane & 15, c = lane >> 4;
-    auto load = [&](int r, int blk, u32x4& lo, u32x4& hi) {
+struct QueryCodes {
+    static constexpr int NB = D / 64;                 // 64-channel blocks
+    u32x4 x[NB][2];
+
+    __device__ __forceinline__ static void load(const char* q, int64_t token_bytes, int G, int r, int lane, u32x4 (&x)[NB][2]) {
         const int t = r / G;
-        const char* src = q + t * token_bytes + (r - t * G) * (D * 2) + (blk * 64 + c * 16) * 2;
-        lo = *reinterpret_cast<const u32x4*>(src);
-        hi = *reinterpret_cast<const u32x4*>(src + 16);
-    };
-    float amax = 0.0f;
-    for (int r = col; r < rows; r += 16) {
+        const char* src = q + t * token_bytes + (r - t * G) * (D * 2) + (lane >> 4) * 32;
 #pragma unroll
         for (int blk = 0; blk < NB; ++blk) {
-            u32x4 lo, hi;
-            load(r, blk, lo, hi);
-            amax = fmaxf(amax, fmaxf(chunk_amax(lo), chunk_amax(hi)));
+            x[blk][0] = *reinterpret_cast<const u32x4*>(src + blk * 128);
+            x[blk][1] = *reinterpret_cast<const u32x4*>(src + blk * 128 + 16);
         }
     }
-    amax = wave_max(amax);
-    // f: smallest with amax <= 127 * 2^f; a group of zeros: any
-    const uint32_t u = __float_as_uint(amax);
-    const int ex = (int)(u >> 23) - 127, f = (u & 0x7fffffu) <= 0x7e0000u ? ex - 6 : ex - 5;
-    const int fs = max(-126, min(127, -f));           // 2^-f in two factors: f reaches -138 and 122
-    const float m0 = __uint_as_float((uint32_t)(fs + 127) << 23), m1 = __uint_as_float((uint32_t)(max(-126, min(127, -f - fs)) + 127) << 23);
-    uint32_t sum[NB][16];                             // positive | negative << 16
+    __device__ __forceinline__ void start(const char* q, int64_t token_bytes, int G, int rows, int lane) {
+        load(q, token_bytes, G, min(lane & 15, rows - 1), lane, x);       // (a lane without a row: the last one's once more, not counted)
+    }
+    __device__ __forceinline__ static uint32_t magnitude(const u32x4 (&v)[NB][2]) {
+        uint32_t m = 0;                               // two 16-bit magnitudes
 #pragma unroll
-    for (int blk = 0; blk < NB; ++blk)
+        for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum[blk][i] = 0;
-    for (int r = col; r < rows; r += 16) {
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) m = max16x2(m, v[blk][half][w] & 0x7fff7fffu);
+        return m;
+    }
+    __device__ __forceinline__ void finish(const char* q, int64_t token_bytes, int G, int rows, int lane, i32x4 (&limb)[2][D / 32]) const {
+        const int col = lane & 15;
+        uint32_t m = magnitude(x);
+        for (int r = col + 16; r < rows; r += 16) {
+            u32x4 y[NB][2];
+            load(q, token_bytes, G, r, lane, y);
+            m = max16x2(m, magnitude(y));
+        }
+        float m0, m1;
+        query_step(wave_umax(max(m >> 16, m & 0xffffu)) << 16, m0, m1);
+        uint32_t sum[NB][16];                         // positive | negative << 16
+        auto add = [&](const u32x4 (&v)[NB][2], bool first) {
+#pragma unroll
+            for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float y[8];
+                    unpack8(v[blk][half], y);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int c = (int)fminf(fmaxf(rintf(y[i] * m0 * m1), -127.0f), 127.0f);
+                        const uint32_t one = c >= 0 ? (uint32_t)c : (uint32_t)(-c) << 16;
+                        sum[blk][half * 8 + i] = first ? one : sum[blk][half * 8 + i] + one;
+                    }
+                }
+        };
+        add(x, true);
+        if (rows < 16 && col >= rows) {
+#pragma unroll
+            for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[blk][i] = 0;
+        }
+        for (int r = col + 16; r < rows; r += 16) {
+            u32x4 y[NB][2];
+            load(q, token_bytes, G, r, lane, y);
+            add(y, false);
+        }
 #pragma unroll
         for (int blk = 0; blk < NB; ++blk) {
-            u32x4 lo, hi;
-            load(r, blk, lo, hi);
-            float v[8];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                unpack8(half ? hi : lo, v);
+            for (int w = 0; w < 4; ++w) {
+                // bytes of four channels: the low 7 bits and the rest, of the positive sums and, negated, of the negative ones
+                uint32_t pl = 0, ph = 0, nl = 0, nh = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int x = (int)fminf(fmaxf(rintf(v[i] * m0 * m1), -127.0f), 127.0f);
-                    sum[blk][half * 8 + i] += x >= 0 ? (uint32_t)x : (uint32_t)(-x) << 16;
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t s = row_sum(sum[blk][w * 4 + i]), lo = s & 0x007f007fu, hi = (s >> 7) & 0x007f007fu;
+                    pl |= (lo & 0xff) << (8 * i);
+                    nl |= (lo >> 16) << (8 * i);
+                    ph |= (hi & 0xff) << (8 * i);
+                    nh |= (hi >> 16) << (8 * i);
                 }
+                limb[0][blk][w] = (int)pl;
+                limb[1][blk][w] = (int)ph;
+                limb[0][NB + blk][w] = (int)negate_bytes(nl);
+                limb[1][NB + blk][w] = (int)negate_bytes(nh);
             }
         }
     }
+};
+
+// The same numbers for the dot products of single-token rows: lane l holds bytes 16 (l % LPP) .. of the 2d (LPP = 2d / 16 lanes to a page), so that a
+// load of 64 lanes takes whole neighbouring bytes of 64 / LPP pages.  As the second operand of a matrix product every load would touch 16 pages
+// for half a line each (96 rows of 2-16 k tokens: 38 us).
+template <int D>
+struct RowCodes {
+    static constexpr int LPP = D / 8, PPI = 64 / LPP;
+    u32x4 x[2];
+    __device__ __forceinline__ static void load(const char* q, int64_t token_bytes, int G, int r, int lane, u32x4 (&x)[2]) {
+        const int t = r / G;
+        const char* src = q + t * token_bytes + (r - t * G) * (D * 2) + (lane % (D / 16)) * 32;
+        x[0] = *reinterpret_cast<const u32x4*>(src);
+        x[1] = *reinterpret_cast<const u32x4*>(src + 16);
+    }
+    __device__ __forceinline__ void start(const char* q, int64_t token_bytes, int G, int rows, int lane) {
+        load(q, token_bytes, G, min(lane / LPP, rows - 1), lane, x);      // (a lane without a row: the last one's once more, not counted)
+    }
+    // limb[l]: 16 bytes of limb l
+    __device__ __forceinline__ void finish(const char* q, int64_t token_bytes, int G, int rows, int lane, i32x4 (&limb)[2]) const {
+        const bool neg = lane % LPP >= D / 16;
+        auto magnitude = [](const u32x4 (&v)[2]) {
+            uint32_t m = 0;
 #pragma unroll
-    for (int blk = 0; blk < NB; ++blk) {
+            for (int w = 0; w < 8; ++w) m = max16x2(m, v[w >> 2][w & 3] & 0x7fff7fffu);
+            return m;
+        };
+        uint32_t m = magnitude(x);
+        for (int r = lane / LPP + PPI; r < rows; r += PPI) {
+            u32x4 y[2];
+            load(q, token_bytes, G, r, lane, y);
+            m = max16x2(m, magnitude(y));
+        }
+        float m0, m1;
+        query_step(wave_umax(max(m >> 16, m & 0xffffu)) << 16, m0, m1);
+        const float least = neg ? -127.0f : 0.0f, most = neg ? 0.0f : 127.0f;
+        uint32_t sum[8];                              // two channels each
+        auto add = [&](const u32x4 (&v)[2], bool first) {
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                const uint32_t u = v[w >> 2][w & 3];
+                const float a = fminf(fmaxf(rintf(__uint_as_float(u << 16) * m0 * m1), least), most);
+                const float b = fminf(fmaxf(rintf(__uint_as_float(u & 0xffff0000u) * m0 * m1), least), most);
+                const uint32_t one = (uint32_t)fabsf(a) | (uint32_t)fabsf(b) << 16;
+                sum[w] = first ? one : sum[w] + one;
+            }
+        };
+        add(x, true);
+        if (lane / LPP >= rows) {
+#pragma unroll
+            for (int w = 0; w < 8; ++w) sum[w] = 0;
+        }
+        for (int r = lane / LPP + PPI; r < rows; r += PPI) {
+            u32x4 y[2];
+            load(q, token_bytes, G, r, lane, y);
+            add(y, false);
+        }
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            if constexpr (LPP == 8) sum[w] = add_dpp<0x128>(sum[w]);      // row_ror:8
+            u32x2 r = __builtin_amdgcn_permlane16_swap(sum[w], sum[w], false, false);
+            const uint32_t t = r[0] + r[1];
+            r = __builtin_amdgcn_permlane32_swap(t, t, false, false);
+            sum[w] = r[0] + r[1];
+        }
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            uint32_t pl = 0, ph = 0, nl = 0, nh = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t s = row_sum(sum[blk][w * 4 + i]), pos = s & 0xffff, neg = s >> 16;
-                pl |= (pos & 127) << (8 * i);
-                ph |= (pos >> 7) << (8 * i);
-                nl |= ((0u - (neg & 127)) & 0xff) << (8 * i);
-                nh |= ((0u - (neg >> 7)) & 0xff) << (8 * i);
-            }
-            limb[0][blk][w] = (int)pl;
-            limb[1][blk][w] = (int)ph;
-            limb[0][NB + blk][w] = (int)nl;
-            limb[1][NB + blk][w] = (int)nh;
+            const uint32_t a = sum[2 * w], b = sum[2 * w + 1];
+            const uint32_t lo = __builtin_amdgcn_perm(b & 0x007f007fu, a & 0x007f007fu, 0x06040200u);
+            const uint32_t hi = __builtin_amdgcn_perm((b >> 7) & 0x007f007fu, (a >> 7) & 0x007f007fu, 0x06040200u);
+            limb[0][w] = (int)(neg ? negate_bytes(lo) : lo);
+            limb[1][w] = (int)(neg ? negate_bytes(hi) : hi);
         }
     }
-}
+};
 
 // A wave per group and KV head: the operand bytes, for the score launch's tiles of 16 groups.
 template <int D>
 __global__ __launch_bounds__(64) void query_codes_kernel(const SelectParams p) {
     const int lane = threadIdx.x, item = blockIdx.x, h = blockIdx.y, G = p.Hq / p.Hkv;
-    const SelectRow r = p.rows[row_of(p, SELECT_MAX_REQS, item, [](const SelectRow& x) { return x.item0; })];
+    const SelectRow r = row_of<SELECT_MAX_REQS>(p.rows, p.n, item, [](const SelectRow& x) { return x.item0; });
     const int tok0 = (item - r.item0) * p.g, m = min(p.g, r.L - tok0);
     const char* q = static_cast<const char*>(p.q) + ((int64_t)(r.row_off + tok0) * p.Hq + h * G) * (D * 2);
     i32x4 limb[2][D / 32];
-    quantise_queries<D>(q, (int64_t)p.Hq * D * 2, G, m * G, lane, limb);
+    QueryCodes<D> qc;
+    qc.start(q, (int64_t)p.Hq * D * 2, G, m * G, lane);
+    qc.finish(q, (int64_t)p.Hq * D * 2, G, m * G, lane, limb);
     if ((lane & 15) == 0) {
         int8_t* dst = p.qcodes + ((int64_t)item * p.Hkv + h) * (4 * D) + (lane >> 4) * 16;
 #pragma unroll
@@ -529,258 +689,333 @@ __device__ __forceinline__ uint32_t ordered(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Scores of 16 groups x 16 pages at a time: the 16x16x64 whole-number product with the groups' queries as one operand and the pages' bounds
-// as the other (both with k = 0..2d-1: largest, then smallest), once per limb.  A wave goes through SCORE_TILES tiles of one KV head; the
-// waves of a workgroup are neighbouring heads of the same pages (a page's bounds of all heads lie next to each other), then
-// neighbouring pages.  ONE: every row of the launch has one group, whose queries the wave quantises itself.
-template <int D, bool ONE>
-__global__ __launch_bounds__(64 * SCORE_WAVES) void page_scores_kernel(const SelectParams p, int heads) {
-    constexpr int KK = D / 32;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const SelectRow r = p.rows[row_of(p, SELECT_MAX_REQS, blockIdx.x, [](const SelectRow& x) { return x.tile0; })];
-    const int G = p.Hq / p.Hkv, per_wg = SCORE_TILES * 16 * (SCORE_WAVES / heads);
-    const int h = blockIdx.y * heads + wave % heads;
-    const int ng = (r.L + p.g - 1) / p.g, tiles = (ng + 15) >> 4, at = blockIdx.x - r.tile0, tile = at % tiles, block = at / tiles;
-    if (h >= p.Hkv) return;
-    // pages that the tile's last group may choose by score
-    const int last_group = min(ng, tile * 16 + 16) - 1;
-    const int end = ((r.C + last_group * p.g) >> p.logP) - p.last + 1;
-    const int pg0 = block * per_wg + (wave / heads) * (SCORE_TILES * 16);
-    if (pg0 >= end) return;
-    const int32_t* bt = p.block_table + (int64_t)r.req * p.max_pages;
-    const int col = lane & 15, c = lane >> 4;
-    int id[SCORE_TILES];
+// A tile of 16 pages: their bounds of one KV head, as the second operand of the 16x16x64 whole-number product (lane l: bytes 16 (l / 16) .. of
+// k-block kk of page l % 16; k = 0..2d-1: the largest keys' codes, then the smallest ones').
+template <int D>
+struct PageTile {
+    i32x4 b[D / 32];
+    float scale;
+    __device__ __forceinline__ void load(const SelectParams& p, int id, int h, int lane) {
+        const int64_t ph = (int64_t)((uint32_t)id < (uint64_t)p.num_pages ? id : 0) * p.Hkv + h;
+        const int8_t* src = p.codes + ph * (2 * D) + (lane >> 4) * 16;
 #pragma unroll
-    for (int t = 0; t < SCORE_TILES; ++t) {
-        id[t] = bt[min(pg0 + t * 16 + col, end - 1)];
-        if ((uint32_t)id[t] >= (uint64_t)p.num_pages) id[t] = 0;
+        for (int kk = 0; kk < D / 32; ++kk) b[kk] = *reinterpret_cast<const i32x4*>(src + kk * 64);
+        scale = p.bscale[ph];
     }
-    i32x4 limb[2][KK];
-    if constexpr (ONE) {
-        quantise_queries<D>(static_cast<const char*>(p.q) + ((int64_t)r.row_off * p.Hq + h * G) * (D * 2), (int64_t)p.Hq * D * 2, G, r.L * G, lane, limb);
-        if (col != 0) {
+    // the groups' queries (first operand, lane l: group l % 16) times the bounds, once per limb: lane l holds page l % 16 and groups 4 (l / 16) + i
+    __device__ __forceinline__ void score(const i32x4 (&limb)[2][D / 32], uint32_t (&key)[4]) const {
+        i32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
 #pragma unroll
-            for (int l = 0; l < 2; ++l)
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk) limb[l][kk] = i32x4{0, 0, 0, 0};
+        for (int kk = 0; kk < D / 32; ++kk) {
+            lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(limb[0][kk], b[kk], lo, 0, 0, 0);
+            hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(limb[1][kk], b[kk], hi, 0, 0, 0);
         }
-    } else {
-        const int item = r.item0 + min(tile * 16 + col, ng - 1);        // (a group behind the last: the last one's, not stored)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key[i] = ordered((float)(hi[i] * 128 + lo[i]) * scale);
+    }
+};
+
+// Where a wave of a score launch works: the waves of a workgroup are `heads` neighbouring KV heads of the same pages (a page's bounds of all
+// heads lie next to each other), then neighbouring pages; a wave takes p.score_tiles tiles of 16 pages.
+struct ScorePlace {
+    SelectRow r;
+    int h, ng, tile, pg0, end;                        // KV head; groups of the row; its tile of 16 groups; the wave's pages
+    __device__ __forceinline__ bool find(const SelectParams& p, int heads, int wave) {
+        r = row_of<SELECT_MAX_REQS>(p.rows, p.n, blockIdx.x, [](const SelectRow& x) { return x.tile0; });
+        const int per_wave = p.score_tiles * 16, per_wg = per_wave * (SCORE_WAVES / heads);
+        h = blockIdx.y * heads + wave % heads;
+        ng = (r.L + p.g - 1) / p.g;
+        const int tiles = (ng + 15) >> 4, at = blockIdx.x - r.tile0, block = at / tiles;
+        tile = at - block * tiles;
+        // pages that the tile's last group may choose by score
+        const int last_group = min(ng, tile * 16 + 16) - 1;
+        pg0 = block * per_wg + (wave / heads) * per_wave;
+        end = min(pg0 + per_wave, ((r.C + last_group * p.g) >> p.logP) - p.last + 1);
+        return h < p.Hkv && pg0 < end;
+    }
+    __device__ __forceinline__ int64_t stride(const SelectParams& p) const { return (((int64_t)r.C + r.L + p.P - 1) / p.P + 63) / 64 * 64; }
+};
+
+// Rows of one group each (decode steps).  A load of 64 lanes takes the bounds of PPI pages of one KV head, a lane 16 of a page's 2d bytes; four
+// or eight whole-number dot products of 4 per limb and a sum over the page's lanes make its score.  The wave quantises the row's queries itself,
+// while its first pages travel.
+template <int D>
+__global__ __launch_bounds__(64 * SCORE_WAVES) void row_scores_kernel(const SelectParams p, int heads) {
+    constexpr int LPP = RowCodes<D>::LPP, PPI = RowCodes<D>::PPI, NL = 16 / PPI, TB = SCORE_BATCH;   // loads per tile; tiles in flight
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    ScorePlace w;
+    if (!w.find(p, heads, wave)) return;
+    const int G = p.Hq / p.Hkv, h = w.h, end = w.end;
+    const int32_t* bt = p.block_table + (int64_t)w.r.req * p.max_pages;
+    // lane's page of a tile: load i = lane % LPP (lanes from NL on: the last load's) brings page i * PPI + lane / LPP to the lane's LPP lanes
+    const int mine = min(lane % LPP, NL - 1) * PPI + lane / LPP;
+    auto page_id = [&](int first) {
+        const int id = bt[min(first + mine, end - 1)];
+        return (uint32_t)id < (uint64_t)p.num_pages ? id : 0;
+    };
+    int id[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) id[t] = page_id(w.pg0 + t * 16);
+    RowCodes<D> qc;
+    const char* q = static_cast<const char*>(p.q) + ((int64_t)w.r.row_off * p.Hq + h * G) * (D * 2);
+    qc.start(q, (int64_t)p.Hq * D * 2, G, w.r.L * G, lane);
+    i32x4 limb[2];
+    uint32_t* keys = p.keys + (int64_t)w.r.key0 * 64 + h * w.stride(p);
+    for (int at = w.pg0; at < end; at += TB * 16) {
+        i32x4 b[TB][NL];
+        float scale[TB];
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int page = __shfl(id[t], (lane & ~(LPP - 1)) + i, 64);
+                b[t][i] = *reinterpret_cast<const i32x4*>(p.codes + ((int64_t)page * p.Hkv + h) * (2 * D) + (lane % LPP) * 16);
+            }
+            scale[t] = p.bscale[(int64_t)id[t] * p.Hkv + h];
+        }
+#pragma unroll
+        for (int t = 0; t < TB; ++t) id[t] = page_id(at + (TB + t) * 16);
+        if (at == w.pg0) {                            // uniform
+            __builtin_amdgcn_sched_barrier(0);
+            qc.finish(q, (int64_t)p.Hq * D * 2, G, w.r.L * G, lane, limb);
+        }
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                int lo = 0, hi = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    lo = __builtin_amdgcn_sdot4(limb[0][k], b[t][i][k], lo, false);
+                    hi = __builtin_amdgcn_sdot4(limb[1][k], b[t][i][k], hi, false);
+                }
+                uint32_t s = (uint32_t)(hi * 128 + lo);
+                s = add_dpp<0xB1>(s);
+                s = add_dpp<0x4E>(s);
+                // (the four lanes of a quad hold its sum: a mirrored half row is the other quad, a rotation by 8 the other half)
+                s = add_dpp<0x141>(s);                // row_half_mirror
+                if constexpr (LPP == 16) s = add_dpp<0x128>(s);           // row_ror:8
+                n = i == lane % LPP ? (int)s : n;
+            }
+            const int page = at + t * 16 + mine;
+            if (lane % LPP < NL && page < end) keys[page] = ordered((float)n * scale[t]);
+        }
+    }
+}
+
+// Scores of 16 groups x 16 pages at a time, SCORE_BATCH tiles in flight at once.
+template <int D>
+__global__ __launch_bounds__(64 * SCORE_WAVES) void page_scores_kernel(const SelectParams p, int heads) {
+    constexpr int KK = D / 32, TB = SCORE_BATCH;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    ScorePlace w;
+    if (!w.find(p, heads, wave)) return;
+    const int h = w.h, end = w.end, col = lane & 15, c = lane >> 4;
+    const int32_t* bt = p.block_table + (int64_t)w.r.req * p.max_pages;
+    int id[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) id[t] = bt[min(w.pg0 + t * 16 + col, end - 1)];
+    i32x4 limb[2][KK];
+    {
+        const int item = w.r.item0 + min(w.tile * 16 + col, w.ng - 1);    // (a group behind the last: the last one's, not stored)
         const int8_t* src = p.qcodes + ((int64_t)item * p.Hkv + h) * (4 * D) + c * 16;
 #pragma unroll
         for (int l = 0; l < 2; ++l)
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) limb[l][kk] = *reinterpret_cast<const i32x4*>(src + l * (2 * D) + kk * 64);
     }
-    const int64_t stride = (((int64_t)r.C + r.L + p.P - 1) / p.P + 63) / 64 * 64;
-    uint32_t* keys = p.keys + (int64_t)r.key0 * 64 + h * stride;
+    const int64_t stride = w.stride(p);
+    uint32_t* keys = p.keys + (int64_t)w.r.key0 * 64 + h * stride;
+    for (int at = w.pg0; at < end; at += TB * 16) {
+        PageTile<D> b[TB];
 #pragma unroll
-    for (int t = 0; t < SCORE_TILES; ++t) {
-        const int64_t ph = (int64_t)id[t] * p.Hkv + h;
-        const int8_t* src = p.codes + ph * (2 * D) + c * 16;
-        i32x4 b[KK];
+        for (int t = 0; t < TB; ++t) b[t].load(p, id[t], h, lane);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) b[kk] = *reinterpret_cast<const i32x4*>(src + kk * 64);
-        const float scale = p.bscale[ph];
-        i32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+        for (int t = 0; t < TB; ++t) id[t] = bt[min(at + (TB + t) * 16 + col, end - 1)];
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-            lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(limb[0][kk], b[kk], lo, 0, 0, 0);
-            hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(limb[1][kk], b[kk], hi, 0, 0, 0);
-        }
-        const int page = pg0 + t * 16 + col;
+        for (int t = 0; t < TB; ++t) {
+            uint32_t key[4];
+            b[t].score(limb, key);
+            const int page = at + t * 16 + col;
 #pragma unroll
-        for (int i = 0; i < (ONE ? 1 : 4); ++i) {
-            const int g = ONE ? 0 : tile * 16 + c * 4 + i;
-            if (page < end && (ONE ? c == 0 : g < ng))
-                keys[(int64_t)g * p.Hkv * stride + page] = ordered((float)(hi[i] * 128 + lo[i]) * scale);
+            for (int i = 0; i < 4; ++i) {
+                const int g = w.tile * 16 + c * 4 + i;
+                if (page < end && g < w.ng) keys[(int64_t)g * p.Hkv * stride + page] = key[i];
+            }
         }
     }
 }
 
-// Of n keys the `need` largest, the lowest index among equals, for one group and KV head; then the list in ascending order.
-// The keys' range is cut into 2 048 bins that are counted; the bin in which the need-th largest lies is cut again while it holds more than
-// LIST keys, whose ranks among themselves settle it otherwise.  (Bins of the leading bits would hold nearly everything in one: scores
-// of one row have few exponents.)  KPT keys per thread stay in registers; KPT = 0: more keys than that, read again in every pass.
-constexpr int SELECT_BINS = 2048, SELECT_LIST = 256;
-template <int NT, int KPT>
-__global__ __launch_bounds__(NT) void choose_pages_kernel(const SelectParams p) {
-    constexpr int NWV = NT / 64, BPT = SELECT_BINS / NT;
-    __shared__ uint32_t bins[SELECT_BINS];
-    __shared__ uint32_t lkey[SELECT_LIST];
-    __shared__ int lidx[SELECT_LIST], lcount, pick[3];
-    __shared__ uint32_t wred[2][NWV];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// What a group chooses from, for any KV head: pages [0, nfirst) and [cend, lp1] always, `need` of the n from cbeg = nfirst on.
+struct Choice {
+    int nfirst, cend, lp1, n, need;
+    __device__ __forceinline__ Choice(const SelectParams& p, const SelectRow& r, int tok0) {
+        const int m = min(p.g, r.L - tok0), lp0 = (r.C + tok0) >> p.logP;
+        lp1 = (r.C + tok0 + m - 1) >> p.logP;
+        nfirst = min(p.first, lp1 + 1);
+        cend = max(nfirst, lp0 - p.last + 1);
+        n = cend - nfirst;
+        need = min(n, p.budget - nfirst - (lp1 + 1 - cend));
+    }
+    // the part of the list that needs no scores, by thread t of nt
+    __device__ __forceinline__ void write_always(int32_t* out, int budget, int t, int nt) const {
+        const int total = nfirst + need + lp1 + 1 - cend;
+        for (int i = t; i < budget; i += nt) {
+            if (i < nfirst) out[i] = i;
+            else if (i >= nfirst + need) out[i] = i < total ? cend + i - nfirst - need : -1;
+            else if (need == n) out[i] = i;
+        }
+    }
+    __device__ __forceinline__ bool nothing_to_choose() const { return need == n || need == 0; }
+};
+
+__device__ __forceinline__ int lanes_below(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
+
+// Sums over the lanes up to and with this one.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane) {
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true);     // row_shr:1, 2, 4, 8
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true);
+    const uint32_t a = __builtin_amdgcn_readlane(x, 15), b = __builtin_amdgcn_readlane(x, 31), c = __builtin_amdgcn_readlane(x, 47);
+    return x + (lane >= 16 ? a : 0u) + (lane >= 32 ? b : 0u) + (lane >= 48 ? c : 0u);
+}
+
+// Of n keys the `need` largest, the lowest index among equals, for one group and KV head, written as page indices in ascending order.
+// The keys' range is cut into 512 bins that are counted in LDS; the bin in which the need-th largest lies is cut again until it is chosen
+// whole or holds one value.  (Bins of the leading bits would hold nearly everything in one: scores of one row have few exponents.  Bisection
+// instead, a count of all keys per step, took 13 to 20 steps and twice as long.)  KPL keys per lane stay in registers; KPL = 0: more keys than that,
+// read again in every pass.  A wave holds a run of neighbouring keys, key i of it in lane i % 64.
+template <int NW, int KPL>
+__global__ __launch_bounds__(64 * NW) void choose_pages_kernel(const SelectParams p) {
+    constexpr int BINS = 512, BPL = BINS / 64;
+    __shared__ __attribute__((aligned(16))) uint32_t bins[BINS];
+    __shared__ uint32_t shared[2][NW];
+    const int lane = threadIdx.x & 63, wave = NW > 1 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : 0;
     const int item = blockIdx.x, h = blockIdx.y;
-    const SelectRow r = p.rows[row_of(p, SELECT_MAX_REQS, item, [](const SelectRow& x) { return x.item0; })];
-    const int grp = item - r.item0, tok0 = grp * p.g, m = min(p.g, r.L - tok0);
-    const int lp0 = (r.C + tok0) >> p.logP, lp1 = (r.C + tok0 + m - 1) >> p.logP;
-    const int nfirst = min(p.first, lp1 + 1), cbeg = nfirst, cend = max(cbeg, lp0 - p.last + 1), ntail = lp1 + 1 - cend;
-    const int n = cend - cbeg, need = min(n, p.budget - nfirst - ntail);
+    const SelectRow r = row_of<SELECT_MAX_REQS>(p.rows, p.n, item, [](const SelectRow& x) { return x.item0; });
+    const int grp = item - r.item0;
+    const Choice ch(p, r, grp * p.g);
     int32_t* out = p.selected + ((int64_t)(r.out0 + grp) * p.Hkv + h) * p.budget;
-    const int total = nfirst + need + ntail;
-    for (int i = tid; i < p.budget; i += NT) {
-        if (i < nfirst) out[i] = i;
-        else if (i >= nfirst + need) out[i] = i < total ? cend + i - nfirst - need : -1;
-        else if (need == n) out[i] = cbeg + i - nfirst;
-    }
-    if (need == n || need == 0) return;               // nothing to choose (uniform)
     const int64_t stride = (((int64_t)r.C + r.L + p.P - 1) / p.P + 63) / 64 * 64;
-    const uint32_t* keys = p.keys + (int64_t)r.key0 * 64 + ((int64_t)grp * p.Hkv + h) * stride + cbeg;
-    const int per = KPT ? KPT : (n + NT - 1) / NT;
-    const int i0 = tid * per;
-    uint32_t reg[KPT ? KPT : 1];
-    if constexpr (KPT > 0) {
+    const int per = KPL ? KPL : (ch.n + 64 * NW - 1) / (64 * NW);         // keys per lane
+    const int i0 = wave * (64 * per), n = min(64 * per, ch.n - i0);       // this wave's first key, and how many it has
+    const uint32_t* src = p.keys + (int64_t)r.key0 * 64 + ((int64_t)grp * p.Hkv + h) * stride + ch.nfirst + i0;
+    uint32_t reg[KPL ? KPL : 1];
+    if constexpr (KPL > 0) {
+        if (!ch.nothing_to_choose()) {
 #pragma unroll
-        for (int i = 0; i < KPT; ++i) reg[i] = i0 + i < n ? keys[i0 + i] : 0u;
+            for (int i = 0; i < KPL; ++i) reg[i] = i * 64 + lane < n ? src[i * 64 + lane] : 0u;
+        }
     }
-    // f(key, index) for this thread's keys
+    ch.write_always(out, p.budget, threadIdx.x, 64 * NW);
+    if (ch.nothing_to_choose()) return;               // uniform
+    // f(key, place in the wave's run, whether there is one)
     auto each = [&](auto&& f) {
-        if constexpr (KPT > 0) {
+        if constexpr (KPL > 0) {
 #pragma unroll
-            for (int i = 0; i < KPT; ++i)
-                if (i0 + i < n) f(reg[i], i0 + i);
+            for (int i = 0; i < KPL; ++i) f(reg[i], i * 64 + lane, i * 64 + lane < n);
         } else {
-            for (int i = i0; i < min(n, i0 + per); ++i) f(keys[i], i);
+            for (int i = 0; i < per; ++i) {
+                const bool there = i * 64 + lane < n;
+                f(there ? src[i * 64 + lane] : 0u, i * 64 + lane, there);
+            }
         }
     };
-    // range of the keys
     uint32_t lo = 0xffffffffu, hi = 0;
-    each([&](uint32_t k, int) {
-        lo = min(lo, k);
+    each([&](uint32_t k, int, bool there) {
+        lo = min(lo, there ? k : 0xffffffffu);
         hi = max(hi, k);
     });
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
-    }
-    if (lane == 0) {
-        wred[0][wave] = lo;
-        wred[1][wave] = hi;
-    }
-    __syncthreads();
-    lo = wred[0][0];
-    hi = wred[1][0];
-    for (int w = 1; w < NWV; ++w) {
-        lo = min(lo, wred[0][w]);
-        hi = max(hi, wred[1][w]);
-    }
-    // keys in (hi, ...] are chosen; of those in [lo, hi] `left` are; the rest is not
-    int left = need;
-    bool all = false;                                 // all of [lo, hi] is chosen
-    bool by_list = false;
-    for (int round = 0; round < 3; ++round) {         // (a range of 32 bits: 21, 10 and 0 are left)
-        const uint32_t range = hi - lo;
-        const int bits = 32 - __clz((int)range);      // (range 0: clz gives 32)
-        const int shift = max(0, bits - 11);
-        for (int i = tid; i < SELECT_BINS; i += NT) bins[i] = 0;
+    lo = wave_umin(lo);
+    hi = wave_umax(hi);
+    if constexpr (NW > 1) {
+        if (lane == 0) {
+            shared[0][wave] = lo;
+            shared[1][wave] = hi;
+        }
         __syncthreads();
-        each([&](uint32_t k, int) {
-            if (k >= lo && k <= hi) atomicAdd(&bins[(k - lo) >> shift], 1u);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            lo = min(lo, shared[0][w]);
+            hi = max(hi, shared[1][w]);
+        }
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    // keys above hi are chosen, `left` of those in [lo, hi], none below; whole: all in [lo, hi] are
+    int left = ch.need;
+    bool whole = false;
+    for (int pass = 0; pass < 4 && lo < hi && !whole; ++pass) {           // (32 bits: 23, 14, 5 and 0 are left)
+        const int shift = max(0, 32 - __clz((int)(hi - lo)) - 9);
+        for (int i = threadIdx.x; i < BINS; i += 64 * NW) bins[i] = 0;
+        __syncthreads();
+        each([&](uint32_t k, int, bool there) {
+            if (there && k >= lo && k <= hi) atomicAdd(&bins[(k - lo) >> shift], 1u);
         });
         __syncthreads();
-        // the bin whose keys and those above it reach `left`: bins from the top, BPT per thread
-        uint32_t mine = 0;
+        // every wave: lane l adds up bins BPL l .. from the top
+        uint32_t b[BPL];
 #pragma unroll
-        for (int b = 0; b < BPT; ++b) mine += bins[SELECT_BINS - 1 - (tid * BPT + b)];
-        uint32_t incl = mine;
+        for (int i = 0; i < BPL; i += 4) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(&bins[BINS - 4 - BPL * lane - i]);
+            b[i] = v.w;
+            b[i + 1] = v.z;
+            b[i + 2] = v.y;
+            b[i + 3] = v.x;
+        }
+        uint32_t sum = 0;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t v = __shfl_up(incl, o, 64);
-            if (lane >= o) incl += v;
+        for (int i = 0; i < BPL; ++i) sum += b[i];
+        const uint32_t upto = wave_scan(sum, lane);
+        uint32_t above = upto - sum;                  // keys in bins above this lane's
+        const uint64_t reach = __ballot(upto >= (uint32_t)left);
+        const int owner = __builtin_ctzll(reach);     // (the keys in [lo, hi] are `left` or more)
+        uint32_t bin = BINS - 1 - BPL * lane, inside = b[0];
+#pragma unroll
+        for (int i = 1; i < BPL; ++i) {
+            const bool on = above + inside < (uint32_t)left;
+            above += on ? inside : 0u;
+            bin -= on ? 1u : 0u;
+            inside = on ? b[i] : inside;
         }
-        if (lane == 63) wred[0][wave] = incl;
-        __syncthreads();
-        uint32_t before = incl - mine;
-        for (int w = 0; w < wave; ++w) before += wred[0][w];
-        if (before < (uint32_t)left && before + mine >= (uint32_t)left) {
-            uint32_t above = before;
-            for (int b = 0; b < BPT; ++b) {
-                const int bin = SELECT_BINS - 1 - (tid * BPT + b);
-                if (above + bins[bin] >= (uint32_t)left) {
-                    pick[0] = bin;
-                    pick[1] = (int)above;
-                    pick[2] = (int)bins[bin];
-                    break;
-                }
-                above += bins[bin];
-            }
-            lcount = 0;
-        }
-        __syncthreads();
-        const int bin = pick[0], inside = pick[2];
-        left -= pick[1];
-        lo += (uint32_t)bin << shift;
+        bin = __builtin_amdgcn_readlane(bin, owner);
+        left -= (int)__builtin_amdgcn_readlane(above, owner);
+        whole = (int)__builtin_amdgcn_readlane(inside, owner) == left;
+        lo += bin << shift;
         hi = min(hi, lo + ((1u << shift) - 1));
-        if (inside == left) {
-            all = true;
-            break;
-        }
-        if (inside <= SELECT_LIST) {
-            by_list = true;
-            break;
-        }
-        if (shift == 0) break;                        // many equal keys: the first `left` of them
-        __syncthreads();
+        if (NW > 1) __syncthreads();                  // before the bins are cleared again
     }
-    if (by_list) {
-        each([&](uint32_t k, int i) {
-            if (k >= lo && k <= hi) {
-                const int s = atomicAdd(&lcount, 1);
-                lkey[s] = k;
-                lidx[s] = i;
-            }
+    if (whole) left = ch.n;
+    int at = ch.nfirst;
+    if constexpr (NW > 1) {                           // what the waves before this one take
+        uint32_t above = 0, equal = 0;
+        each([&](uint32_t k, int, bool there) {
+            above += there && k > hi ? 1u : 0u;
+            equal += there && k >= lo && k <= hi ? 1u : 0u;
         });
-        __syncthreads();
-    }
-    const int inside = pick[2];
-    // how many of this thread's keys are chosen, and of those equal to the border how many it has
-    int count = 0, equal = 0;
-    auto rank_ok = [&](uint32_t k, int i) {           // fewer than `left` of the listed keys come before it
-        int rank = 0;
-        for (int s = 0; s < inside; ++s) rank += lkey[s] > k || (lkey[s] == k && lidx[s] < i) ? 1 : 0;
-        return rank < left;
-    };
-    uint64_t chosen = 0;                              // of this thread's keys (KPT > 0: all fit)
-    each([&](uint32_t k, int i) {
-        bool take = k > hi;
-        if (!take && k >= lo) take = all || (by_list ? rank_ok(k, i) : false);
-        if (!all && !by_list && k >= lo && k <= hi) ++equal;
-        count += take ? 1 : 0;
-        if constexpr (KPT > 0) chosen |= (uint64_t)take << (i - i0);
-    });
-    // exclusive prefixes over the threads
-    auto prefix = [&](int v) {
-        int incl = v;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(incl, o, 64);
-            if (lane >= o) incl += x;
+        above = wave_usum(above);
+        equal = wave_usum(equal);
+        if (lane == 0) {
+            shared[0][wave] = above;
+            shared[1][wave] = equal;
         }
         __syncthreads();
-        if (lane == 63) wred[0][wave] = (uint32_t)incl;
-        __syncthreads();
-        int b = incl - v;
-        for (int w = 0; w < wave; ++w) b += (int)wred[0][w];
-        return b;
-    };
-    int eq_before = 0;
-    if (!all && !by_list) {
-        eq_before = prefix(equal);
-        count += min(max(left - eq_before, 0), equal);
-    }
-    int at = nfirst + prefix(count);
-    each([&](uint32_t k, int i) {
-        bool take;
-        if constexpr (KPT > 0) {
-            take = chosen >> (i - i0) & 1;
-        } else {
-            take = k > hi;
-            if (!take && k >= lo) take = all || (by_list ? rank_ok(k, i) : false);
+        for (int w = 0; w < wave; ++w) {
+            const int take = min(left, (int)shared[1][w]);
+            at += (int)shared[0][w] + take;
+            left -= take;
         }
-        if (!all && !by_list && k >= lo && k <= hi) take = eq_before++ < left;
-        if (take) out[at++] = cbeg + i;
+    }
+    each([&](uint32_t k, int i, bool there) {
+        const bool equal = there && k >= lo && k <= hi;
+        const uint64_t em = __ballot(equal);
+        const bool take = (there && k > hi) || (equal && lanes_below(em) < left);
+        const uint64_t m = __ballot(take);
+        if (take) out[at + lanes_below(m)] = ch.nfirst + i0 + i;
+        at += __popcll(m);
+        left -= min(left, (int)__popcll(em));
     });
 }
 
@@ -790,7 +1025,9 @@ __global__ __launch_bounds__(NT) void choose_pages_kernel(const SelectParams p) 
 // K/V loader of one wave: blocks of 32 keys, two halves of 16 consecutive slots of a page each (global -> registers -> the wave's LDS region).
 // A block's position in the list decides its page; the list entries of the wave's next 8 blocks come with one load, their page ids with
 // another that is made a block later, so that neither is waited for.
-template <int D, int KVT>
+// ONCE: every page is read by one group (rows of one group each): loads that leave no lines behind (96 rows of 128 pages: 144 -> 130 us).  Lists of
+// neighbouring groups share pages, and their lines (64 groups of one row, 42 us, 48 so).
+template <int D, int KVT, bool ONCE>
 struct ListLoader {
     using G_ = Geo<D>;
     using T = LanePlace<D, KVT, 1>;
@@ -848,8 +1085,8 @@ struct ListLoader {
             asm("" : "+v"(lo));
 #pragma unroll
             for (int i = 0; i < LPH; ++i) {
-                k[h * LPH + i].v = *(GlobalChunk)(ka + i * 1024 + lo);
-                v[h * LPH + i].v = *(GlobalChunk)(va + i * 1024 + lo);
+                k[h * LPH + i].v = ONCE ? __builtin_nontemporal_load((GlobalChunk)(ka + i * 1024 + lo)) : *(GlobalChunk)(ka + i * 1024 + lo);
+                v[h * LPH + i].v = ONCE ? __builtin_nontemporal_load((GlobalChunk)(va + i * 1024 + lo)) : *(GlobalChunk)(va + i * 1024 + lo);
             }
         }
         return true;
@@ -892,7 +1129,7 @@ __device__ __forceinline__ bool sparse_item(const SparseParams& p, int ROWS, int
     const int tile = b % p.tiles;
     b /= p.tiles;
     it.group = b;
-    const SparseRow r = p.rows[row_of(p, SPARSE_MAX_REQS, b, [](const SparseRow& x) { return x.first; })];
+    const SparseRow r = row_of<SPARSE_MAX_REQS>(p.rows, p.n, b, [](const SparseRow& x) { return x.first; });
     it.req = r.req;
     it.G = p.Hq / p.Hkv;
     it.tok0 = (b - r.first) * p.g;
@@ -911,7 +1148,7 @@ constexpr int sparse_smem() {
 
 // An item: the rows of a group (tokens x heads of a KV head, ROWS at a time) over a piece of the group's list.  The waves take the piece's
 // blocks of 32 keys in turn, each with a softmax state and an LDS region of its own, and the states are merged at the end.
-template <int D, int KVT, int ROWS, int NW>
+template <int D, int KVT, int ROWS, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparseParams p) {
     using G_ = Geo<D>;
     constexpr bool R16 = ROWS == 16;
@@ -932,7 +1169,7 @@ __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparsePar
     const int32_t* list = p.selected + (it.group * p.Hkv + it.kvh) * p.budget;
     const int32_t* bt = p.block_table + (int64_t)it.req * p.max_pages;
 
-    ListLoader<D, KVT> ld;
+    ListLoader<D, KVT, ONCE> ld;
     if (nj > 0) ld.fetch_entries(p, list, last_page, key0, step, end, 0, lane);
     bf16x8 Q[R16 ? D / 32 : G_::NKK];
     {
@@ -1094,7 +1331,7 @@ __global__ __launch_bounds__(WG) void sparse_join_kernel(const SparseParams p) {
     const float* base = p.partial + (int64_t)it.linear * (ROWS * (D + 2));
     float m = NEG_INF, l = 0.0f;
     f32x4 acc = {0, 0, 0, 0};
-    constexpr int UN = 8;
+    constexpr int UN = 16;                            // (all of them, as a rule)
     for (int s0 = 0; s0 < p.splits; s0 += UN) {
         float mv[UN], lv[UN];
         f32x4 ov[UN];
@@ -1150,8 +1387,9 @@ static void rope_p(const RopeParams& p, unsigned nx, unsigned ny, hipStream_t st
 // max_new: the most new tokens of a page
 hipError_t launch_rope(RopeParams& p, int kvt, int64_t pages, int max_new, hipStream_t st) {
     const int64_t jobs = 2 * p.a.Hkv + (p.q ? ((int64_t)max_new * p.Hq * (p.a.D / 16) + 255) / 256 : 0);
-    // a wave per job while that fills the chip; in long launches the waves of a page share its jobs, and its angles, among fewer
-    const int64_t ny = std::min((jobs + 3) / 4, std::max<int64_t>(1, 2048 / pages));
+    // a wave per job while that fills the chip; in long launches fewer waves share a page's jobs, and its angles, evenly
+    const int64_t least = std::min((jobs + 3) / 4, std::max<int64_t>(1, 2048 / pages)), each = std::max<int64_t>(1, jobs / (4 * least));
+    const int64_t ny = (jobs + 4 * each - 1) / (4 * each);
     for (int64_t at = 0; at < pages; at += MAX_PAGES) {
         p.a.pg0 = (int32_t)at;
         const unsigned nx = (unsigned)std::min(MAX_PAGES, pages - at);
@@ -1166,23 +1404,27 @@ hipError_t launch_rope(RopeParams& p, int kvt, int64_t pages, int max_new, hipSt
     return hipGetLastError();
 }
 
+template <int D, int P, int KVT>
+static void bounds_t(const BoundsParams& p, unsigned nx, hipStream_t st) {
+    hipLaunchKernelGGL((page_bounds_kernel<D, P, KVT>), dim3(nx, (p.a.Hkv + 3) / 4), dim3(WG), 0, st, p);
+}
 template <int D, int KVT>
-static void bounds_p(const BoundsParams& p, dim3 grid, hipStream_t st) {
-    if (p.a.P == 16) hipLaunchKernelGGL((page_bounds_kernel<D, 16, KVT>), grid, dim3(WG), 0, st, p);
-    else if (p.a.P == 32) hipLaunchKernelGGL((page_bounds_kernel<D, 32, KVT>), grid, dim3(WG), 0, st, p);
-    else hipLaunchKernelGGL((page_bounds_kernel<D, 64, KVT>), grid, dim3(WG), 0, st, p);
+static void bounds_p(const BoundsParams& p, unsigned nx, hipStream_t st) {
+    if (p.a.P == 16) bounds_t<D, 16, KVT>(p, nx, st);
+    else if (p.a.P == 32) bounds_t<D, 32, KVT>(p, nx, st);
+    else bounds_t<D, 64, KVT>(p, nx, st);
 }
 
 hipError_t launch_bounds(BoundsParams& p, int kvt, int64_t pages, hipStream_t st) {
     for (int64_t at = 0; at < pages; at += MAX_PAGES) {
         p.a.pg0 = (int32_t)at;
-        const dim3 grid((unsigned)std::min(MAX_PAGES, pages - at), (p.a.Hkv + 3) / 4);
+        const unsigned nx = (unsigned)std::min(MAX_PAGES, pages - at);
         if (p.a.D == 128) {
-            if (kvt == KV_BF16) bounds_p<128, KV_BF16>(p, grid, st);
-            else bounds_p<128, KV_FP8>(p, grid, st);
+            if (kvt == KV_BF16) bounds_p<128, KV_BF16>(p, nx, st);
+            else bounds_p<128, KV_FP8>(p, nx, st);
         } else {
-            if (kvt == KV_BF16) bounds_p<64, KV_BF16>(p, grid, st);
-            else bounds_p<64, KV_FP8>(p, grid, st);
+            if (kvt == KV_BF16) bounds_p<64, KV_BF16>(p, nx, st);
+            else bounds_p<64, KV_FP8>(p, nx, st);
         }
     }
     return hipGetLastError();
@@ -1196,17 +1438,18 @@ static void select_t(const SelectParams& p, int groups, int score_blocks, int64_
         const int heads = score_heads(p.Hkv);
         const dim3 grid(score_blocks, (p.Hkv + heads - 1) / heads);
         if (one) {
-            hipLaunchKernelGGL((page_scores_kernel<D, true>), grid, dim3(64 * SCORE_WAVES), 0, st, p, heads);
+            hipLaunchKernelGGL((row_scores_kernel<D>), grid, dim3(64 * SCORE_WAVES), 0, st, p, heads);
         } else {
             hipLaunchKernelGGL((query_codes_kernel<D>), dim3(groups, p.Hkv), dim3(64), 0, st, p);
-            hipLaunchKernelGGL((page_scores_kernel<D, false>), grid, dim3(64 * SCORE_WAVES), 0, st, p, heads);
+            hipLaunchKernelGGL((page_scores_kernel<D>), grid, dim3(64 * SCORE_WAVES), 0, st, p, heads);
         }
     }
     const dim3 grid(groups, p.Hkv);
-    if (max_keys <= 256 * 4) hipLaunchKernelGGL((choose_pages_kernel<256, 4>), grid, dim3(256), 0, st, p);
-    else if (max_keys <= 256 * 16) hipLaunchKernelGGL((choose_pages_kernel<256, 16>), grid, dim3(256), 0, st, p);
-    else if (max_keys <= 1024 * 16) hipLaunchKernelGGL((choose_pages_kernel<1024, 16>), grid, dim3(1024), 0, st, p);
-    else hipLaunchKernelGGL((choose_pages_kernel<1024, 0>), grid, dim3(1024), 0, st, p);
+    // (a wave alone with 16 keys a lane, and 4 waves with 16: 7.6 us instead of 6.7 for 768 choices of 128 to 1 024 pages, 7.5 instead of 6.0 for 4 of 2 176)
+    if (max_keys <= 4 * 64 * 4) hipLaunchKernelGGL((choose_pages_kernel<4, 4>), grid, dim3(256), 0, st, p);
+    else if (max_keys <= 8 * 64 * 8) hipLaunchKernelGGL((choose_pages_kernel<8, 8>), grid, dim3(512), 0, st, p);
+    else if (max_keys <= 16 * 64 * 16) hipLaunchKernelGGL((choose_pages_kernel<16, 16>), grid, dim3(1024), 0, st, p);
+    else hipLaunchKernelGGL((choose_pages_kernel<16, 0>), grid, dim3(1024), 0, st, p);
 }
 
 // groups: of this launch; score_blocks: workgroup columns of the score launch (0: every group takes all its pages); max_keys: the most pages
@@ -1217,26 +1460,35 @@ hipError_t launch_select(const SelectParams& p, int D, int groups, int score_blo
     return hipGetLastError();
 }
 
-template <int D, int KVT>
-static void sparse_t(const SparseParams& p, int groups, hipStream_t st) {
+template <int D, int KVT, int ROWS, bool ONCE>
+static void sparse_t(const SparseParams& p, int groups, int waves, hipStream_t st) {
     const int64_t items = (int64_t)groups * p.tiles * p.Hkv;
-    const dim3 grid((unsigned)(items * p.splits)), join((unsigned)items, 1);
-    if (sparse_tile(p.g * (p.Hq / p.Hkv)) == 16) {
-        hipLaunchKernelGGL((sparse_rows_kernel<D, KVT, 16, 4>), grid, dim3(256), 0, st, p);
-        if (p.splits > 1) hipLaunchKernelGGL((sparse_join_kernel<D, 16>), dim3((unsigned)items, 16 * D / 4 / WG), dim3(WG), 0, st, p);
+    const dim3 grid((unsigned)(items * p.splits));
+    if (waves == 8) hipLaunchKernelGGL((sparse_rows_kernel<D, KVT, ROWS, 8, ONCE>), grid, dim3(512), 0, st, p);
+    else hipLaunchKernelGGL((sparse_rows_kernel<D, KVT, ROWS, 4, ONCE>), grid, dim3(256), 0, st, p);
+    if (p.splits > 1) hipLaunchKernelGGL((sparse_join_kernel<D, ROWS>), dim3((unsigned)items, ROWS * D / 4 / WG), dim3(WG), 0, st, p);
+}
+template <int D, int KVT>
+static void sparse_k(const SparseParams& p, int groups, int waves, hipStream_t st) {
+    const int rows = p.g * (p.Hq / p.Hkv);
+    bool once = rows <= sparse_tile(rows);
+    for (int i = 0; i < p.n; ++i) once &= p.rows[i].L <= p.g;
+    if (sparse_tile(rows) == 16) {
+        if (once) sparse_t<D, KVT, 16, true>(p, groups, waves, st);
+        else sparse_t<D, KVT, 16, false>(p, groups, waves, st);
     } else {
-        hipLaunchKernelGGL((sparse_rows_kernel<D, KVT, 32, 4>), grid, dim3(256), 0, st, p);
-        if (p.splits > 1) hipLaunchKernelGGL((sparse_join_kernel<D, 32>), dim3((unsigned)items, 32 * D / 4 / WG), dim3(WG), 0, st, p);
+        if (once) sparse_t<D, KVT, 32, true>(p, groups, waves, st);
+        else sparse_t<D, KVT, 32, false>(p, groups, waves, st);
     }
 }
 
-hipError_t launch_sparse(const SparseParams& p, int D, int kvt, int groups, hipStream_t st) {
+hipError_t launch_sparse(const SparseParams& p, int D, int kvt, int groups, int waves, hipStream_t st) {
     if (D == 128) {
-        if (kvt == KV_BF16) sparse_t<128, KV_BF16>(p, groups, st);
-        else sparse_t<128, KV_FP8>(p, groups, st);
+        if (kvt == KV_BF16) sparse_k<128, KV_BF16>(p, groups, waves, st);
+        else sparse_k<128, KV_FP8>(p, groups, waves, st);
     } else {
-        if (kvt == KV_BF16) sparse_t<64, KV_BF16>(p, groups, st);
-        else sparse_t<64, KV_FP8>(p, groups, st);
+        if (kvt == KV_BF16) sparse_k<64, KV_BF16>(p, groups, waves, st);
+        else sparse_k<64, KV_FP8>(p, groups, waves, st);
     }
     return hipGetLastError();
 }

@@ -131,6 +131,7 @@ ampd_status ampd_select_pages(const ampd_kv_cache* cache, const ampd_batch* batc
     p.last = sel->last_pages;
     p.g = sel->group_tokens;
     return select_launches(cache, batch, sel, [&](const SelectLaunch& l) {
+        p.score_tiles = l.score_tiles;
         p.n = l.n;
         std::memcpy(p.rows, l.rows, l.n * sizeof(SelectRow));
         return launch_select(p, cache->head_dim, l.groups, l.score_blocks, l.max_keys, static_cast<hipStream_t>(stream)) == hipSuccess ? AMPD_OK : AMPD_ERR_HIP;
@@ -170,7 +171,7 @@ ampd_status ampd_sparse_attn(const ampd_kv_cache* cache, const ampd_batch* batch
         p.chunk = l.chunk;
         p.n = l.n;
         std::memcpy(p.rows, l.rows, l.n * sizeof(SparseRow));
-        return launch_sparse(p, cache->head_dim, kv_type(cache), l.groups, static_cast<hipStream_t>(stream)) == hipSuccess ? AMPD_OK : AMPD_ERR_HIP;
+        return launch_sparse(p, cache->head_dim, kv_type(cache), l.groups, l.waves, static_cast<hipStream_t>(stream)) == hipSuccess ? AMPD_OK : AMPD_ERR_HIP;
     });
 }
 

@@ -71,9 +71,23 @@ ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const a
     const int64_t most_groups = std::max<int64_t>(1, (1 << 21) / Hkv);        // a grid holds fewer than 2^32 threads
     SelectLaunch l;
     ampd_status st = AMPD_OK;
+    // pages that the last group of a row may choose by score (its other groups: no more), or 0 if it takes all it has
+    auto scored = [&](const SelectRow& x) -> int64_t {
+        const int64_t tok0 = (groups_of(x.L, g) - 1) * g, lp0 = (x.C + tok0) >> logP, lp1 = ((int64_t)x.C + x.L - 1) >> logP, end = lp0 - s->last_pages + 1;
+        return end > s->first_pages && lp1 + 1 > s->budget ? end : 0;
+    };
     auto flush = [&]() {
+        int64_t tiles = 0;
+        for (int i = 0; i < l.n; ++i) tiles += (groups_of(l.rows[i].L, g) + 15) / 16 * ((scored(l.rows[i]) + 15) / 16) * Hkv;
+        l.score_tiles = score_tiles(tiles);
+        const int per = score_pages(Hkv, l.score_tiles);
+        for (int i = 0; i < l.n; ++i) {
+            l.rows[i].tile0 = l.score_blocks;
+            l.score_blocks += (int)((groups_of(l.rows[i].L, g) + 15) / 16 * ((scored(l.rows[i]) + per - 1) / per));
+        }
         if (l.n > 0 && st == AMPD_OK) st = f(l);
-        l = SelectLaunch();
+        l.n = l.groups = l.score_blocks = 0;
+        l.keys = l.max_keys = 0;
     };
     int64_t row_off = 0, out0 = 0;
     for (int r = 0; r < b->num_reqs && st == AMPD_OK; ++r) {
@@ -92,14 +106,10 @@ ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const a
             x.req = r;
             x.out0 = (int32_t)(out0 + at);
             x.item0 = l.groups;
-            x.tile0 = l.score_blocks;
             x.key0 = (uint32_t)(l.keys / 64);
             l.groups += (int)take;
-            // pages that the last group of these may choose by score (the others: no more)
-            const int64_t tok0 = (take - 1) * g, lp0 = (x.C + tok0) >> logP, lp1 = (x.C + x.L - 1) >> logP, end = lp0 - s->last_pages + 1;
-            if (end > s->first_pages && lp1 + 1 > s->budget) {
+            if (const int64_t end = scored(x)) {
                 l.max_keys = std::max(l.max_keys, end - s->first_pages);
-                l.score_blocks += (int)((take + 15) / 16 * ((end + score_pages(Hkv) - 1) / score_pages(Hkv)));
                 l.keys += take * Hkv * key_stride((int64_t)x.C + x.L, P);
             }
             at += take;
@@ -129,8 +139,12 @@ ampd_status sparse_launches(const ampd_kv_cache* c, const ampd_batch* b, int32_t
     auto flush = [&](int64_t next) {
         if (l.n > 0 && st == AMPD_OK) {
             l.tiles = tiles;
-            // Two workgroups of 4 waves to a CU fill the chip: fewer items are cut into pieces, of a block of 32 keys per wave at least.
-            const int64_t items = (int64_t)l.groups * tiles * Hkv, want = std::max<int64_t>(1, 512 / items), least = 4 * 32;
+            // Two workgroups of 4 waves to a CU fill the chip.  Half as many items, down to one for every other CU, go as workgroups of 8 waves
+            // (200 lists of 2 048 keys, 8 bits, d = 64: 16.0 us instead of 16.6 in two pieces and 4.0 for the join); fewer are cut into pieces, of a
+            // block of 32 keys per wave at least.
+            const int64_t items = (int64_t)l.groups * tiles * Hkv;
+            l.waves = items >= 128 && items <= 256 ? 8 : 4;
+            const int64_t want = l.waves == 8 ? 1 : std::max<int64_t>(1, 512 / items), least = l.waves * 32;
             const int64_t per = ((keys + want - 1) / want + least - 1) / least * least;
             l.chunk = (int)per;
             l.splits = (int)((keys + per - 1) / per);
