@@ -95,7 +95,20 @@ ampd_status validate_sparse(const ampd_kv_cache* c, const ampd_batch* b, int32_t
 // f for each launch of a call, in order; the first status that is not AMPD_OK ends it
 ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* sel, LaunchFn<SelectLaunch> f);
 ampd_status sparse_launches(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, int32_t group_tokens, LaunchFn<SparseLaunch> f);
-int64_t select_keys_bytes(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* sel);   // of the keys, in front of the query codes
+// What a call needs of its workspace, and its launch where it has one alone (the usual case: it is then not worked out twice).
+struct SelectPlan {
+    int64_t keys_bytes = 0;   // of the keys; the query codes follow
+    int64_t bytes = 0;
+    int launches = 0;
+    SelectLaunch only;
+};
+void select_plan(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* sel, SelectPlan* out);
+struct SparsePlan {
+    int64_t bytes = 0;
+    int launches = 0;
+    SparseLaunch only;
+};
+void sparse_plan(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, int32_t group_tokens, SparsePlan* out);
 
 }  // namespace host
 

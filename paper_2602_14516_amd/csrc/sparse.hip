@@ -500,13 +500,13 @@ __device__ __forceinline__ void query_step(uint32_t amax_bits, float& m0, float&
 // Whole numbers of a group's queries for one KV head, summed over its rows (tokens x heads), as two limbs of 7 bits in the operand layout of
 // the 16x16x64 product: lane l holds bytes 16 (l / 16) .. of k-block kk; k = 0..d-1 the sums of the positive parts, d..2d-1 of the
 // negative ones.  Every lane of a row of 16 ends up with the same.  At most 128 rows of at most 127 each: sums below 2^14.
-// The lanes of a row of 16 take the group's rows in turn; start() fetches the first 16, so that other loads can be issued behind them.
+// The lanes of a row of 16 take the group's rows in turn, the first 32 in flight at once.
 template <int D>
-struct QueryCodes {
-    static constexpr int NB = D / 64;                 // 64-channel blocks
-    u32x4 x[NB][2];
-
-    __device__ __forceinline__ static void load(const char* q, int64_t token_bytes, int G, int r, int lane, u32x4 (&x)[NB][2]) {
+__device__ __forceinline__ void quantise_queries(const char* q, int64_t token_bytes, int G, int rows, int lane, i32x4 (&limb)[2][D / 32]) {
+    constexpr int NB = D / 64;                        // 64-channel blocks
+    const int col = lane & 15;
+    auto load = [&](int r, u32x4 (&x)[NB][2]) {       // (a lane without a row: the last one's once more, not counted)
+        r = min(r, rows - 1);
         const int t = r / G;
         const char* src = q + t * token_bytes + (r - t * G) * (D * 2) + (lane >> 4) * 32;
 #pragma unroll
@@ -514,11 +514,8 @@ struct QueryCodes {
             x[blk][0] = *reinterpret_cast<const u32x4*>(src + blk * 128);
             x[blk][1] = *reinterpret_cast<const u32x4*>(src + blk * 128 + 16);
         }
-    }
-    __device__ __forceinline__ void start(const char* q, int64_t token_bytes, int G, int rows, int lane) {
-        load(q, token_bytes, G, min(lane & 15, rows - 1), lane, x);       // (a lane without a row: the last one's once more, not counted)
-    }
-    __device__ __forceinline__ static uint32_t magnitude(const u32x4 (&v)[NB][2]) {
+    };
+    auto magnitude = [](const u32x4 (&v)[NB][2]) {
         uint32_t m = 0;                               // two 16-bit magnitudes
 #pragma unroll
         for (int blk = 0; blk < NB; ++blk)
@@ -527,67 +524,67 @@ struct QueryCodes {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) m = max16x2(m, v[blk][half][w] & 0x7fff7fffu);
         return m;
+    };
+    u32x4 x0[NB][2], x1[NB][2];
+    load(col, x0);
+    if (rows > 16) load(col + 16, x1);                // uniform
+    uint32_t m = magnitude(x0);
+    if (rows > 16) m = max16x2(m, magnitude(x1));
+    for (int r = 32; r < rows; r += 16) {
+        u32x4 y[NB][2];
+        load(r + col, y);
+        m = max16x2(m, magnitude(y));
     }
-    __device__ __forceinline__ void finish(const char* q, int64_t token_bytes, int G, int rows, int lane, i32x4 (&limb)[2][D / 32]) const {
-        const int col = lane & 15;
-        uint32_t m = magnitude(x);
-        for (int r = col + 16; r < rows; r += 16) {
-            u32x4 y[NB][2];
-            load(q, token_bytes, G, r, lane, y);
-            m = max16x2(m, magnitude(y));
-        }
-        float m0, m1;
-        query_step(wave_umax(max(m >> 16, m & 0xffffu)) << 16, m0, m1);
-        uint32_t sum[NB][16];                         // positive | negative << 16
-        auto add = [&](const u32x4 (&v)[NB][2], bool first) {
+    float m0, m1;
+    query_step(wave_umax(max(m >> 16, m & 0xffffu)) << 16, m0, m1);
+    uint32_t sum[NB][16];                             // positive | negative << 16
 #pragma unroll
-            for (int blk = 0; blk < NB; ++blk)
+    for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float y[8];
-                    unpack8(v[blk][half], y);
+        for (int i = 0; i < 16; ++i) sum[blk][i] = 0;
+    auto add = [&](const u32x4 (&v)[NB][2], bool there) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int c = (int)fminf(fmaxf(rintf(y[i] * m0 * m1), -127.0f), 127.0f);
-                        const uint32_t one = c >= 0 ? (uint32_t)c : (uint32_t)(-c) << 16;
-                        sum[blk][half * 8 + i] = first ? one : sum[blk][half * 8 + i] + one;
-                    }
+        for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float y[8];
+                unpack8(v[blk][half], y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = (int)fminf(fmaxf(rintf(y[i] * m0 * m1), -127.0f), 127.0f);
+                    const uint32_t one = c >= 0 ? (uint32_t)c : (uint32_t)(-c) << 16;
+                    sum[blk][half * 8 + i] += there ? one : 0u;
                 }
-        };
-        add(x, true);
-        if (rows < 16 && col >= rows) {
-#pragma unroll
-            for (int blk = 0; blk < NB; ++blk)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum[blk][i] = 0;
-        }
-        for (int r = col + 16; r < rows; r += 16) {
-            u32x4 y[NB][2];
-            load(q, token_bytes, G, r, lane, y);
-            add(y, false);
-        }
-#pragma unroll
-        for (int blk = 0; blk < NB; ++blk) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                // bytes of four channels: the low 7 bits and the rest, of the positive sums and, negated, of the negative ones
-                uint32_t pl = 0, ph = 0, nl = 0, nh = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t s = row_sum(sum[blk][w * 4 + i]), lo = s & 0x007f007fu, hi = (s >> 7) & 0x007f007fu;
-                    pl |= (lo & 0xff) << (8 * i);
-                    nl |= (lo >> 16) << (8 * i);
-                    ph |= (hi & 0xff) << (8 * i);
-                    nh |= (hi >> 16) << (8 * i);
-                }
-                limb[0][blk][w] = (int)pl;
-                limb[1][blk][w] = (int)ph;
-                limb[0][NB + blk][w] = (int)negate_bytes(nl);
-                limb[1][NB + blk][w] = (int)negate_bytes(nh);
             }
+    };
+    add(x0, col < rows);
+    if (rows > 16) add(x1, col + 16 < rows);
+    for (int r = 32; r < rows; r += 16) {
+        u32x4 y[NB][2];
+        load(r + col, y);
+        add(y, r + col < rows);
+    }
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            // bytes of four channels: the low 7 bits and the rest, of the positive sums and, negated, of the negative ones
+            uint32_t pl = 0, ph = 0, nl = 0, nh = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t s = row_sum(sum[blk][w * 4 + i]), lo = s & 0x007f007fu, hi = (s >> 7) & 0x007f007fu;
+                pl |= (lo & 0xff) << (8 * i);
+                nl |= (lo >> 16) << (8 * i);
+                ph |= (hi & 0xff) << (8 * i);
+                nh |= (hi >> 16) << (8 * i);
+            }
+            limb[0][blk][w] = (int)pl;
+            limb[1][blk][w] = (int)ph;
+            limb[0][NB + blk][w] = (int)negate_bytes(nl);
+            limb[1][NB + blk][w] = (int)negate_bytes(nh);
         }
     }
-};
+}
 
 // The same numbers for the dot products of single-token rows: lane l holds bytes 16 (l % LPP) .. of the 2d (LPP = 2d / 16 lanes to a page), so that a
 // load of 64 lanes takes whole neighbouring bytes of 64 / LPP pages.  As the second operand of a matrix product every load would touch 16 pages
@@ -671,9 +668,7 @@ __global__ __launch_bounds__(64) void query_codes_kernel(const SelectParams p) {
     const int tok0 = (item - r.item0) * p.g, m = min(p.g, r.L - tok0);
     const char* q = static_cast<const char*>(p.q) + ((int64_t)(r.row_off + tok0) * p.Hq + h * G) * (D * 2);
     i32x4 limb[2][D / 32];
-    QueryCodes<D> qc;
-    qc.start(q, (int64_t)p.Hq * D * 2, G, m * G, lane);
-    qc.finish(q, (int64_t)p.Hq * D * 2, G, m * G, lane, limb);
+    quantise_queries<D>(q, (int64_t)p.Hq * D * 2, G, m * G, lane, limb);
     if ((lane & 15) == 0) {
         int8_t* dst = p.qcodes + ((int64_t)item * p.Hkv + h) * (4 * D) + (lane >> 4) * 16;
 #pragma unroll

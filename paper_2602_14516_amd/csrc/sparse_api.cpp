@@ -111,7 +111,9 @@ ampd_status ampd_select_pages(const ampd_kv_cache* cache, const ampd_batch* batc
     if ((vs = validate_bounds(bounds)) != AMPD_OK) return vs;
     if (nothing_new(batch)) return AMPD_OK;
     if (!batch->d_block_table || !aligned(q, 16) || !aligned(selected, 4)) return AMPD_ERR_INVALID_ARG;
-    if (!aligned(workspace, 256) || workspace_bytes < ampd_select_pages_workspace_bytes(cache, batch, sel)) return AMPD_ERR_WORKSPACE;
+    SelectPlan plan;
+    select_plan(cache, batch, sel, &plan);
+    if (!aligned(workspace, 256) || workspace_bytes < (size_t)plan.bytes) return AMPD_ERR_WORKSPACE;
     SelectParams p;
     p.q = q;
     p.codes = bounds->codes;
@@ -119,7 +121,7 @@ ampd_status ampd_select_pages(const ampd_kv_cache* cache, const ampd_batch* batc
     p.block_table = batch->d_block_table;
     p.selected = selected;
     p.keys = static_cast<uint32_t*>(workspace);
-    p.qcodes = static_cast<int8_t*>(workspace) + select_keys_bytes(cache, batch, sel);
+    p.qcodes = static_cast<int8_t*>(workspace) + plan.keys_bytes;
     p.num_pages = cache->num_pages;
     p.Hq = cache->num_q_heads;
     p.Hkv = cache->num_kv_heads;
@@ -130,12 +132,13 @@ ampd_status ampd_select_pages(const ampd_kv_cache* cache, const ampd_batch* batc
     p.first = sel->first_pages;
     p.last = sel->last_pages;
     p.g = sel->group_tokens;
-    return select_launches(cache, batch, sel, [&](const SelectLaunch& l) {
+    auto launch = [&](const SelectLaunch& l) {
         p.score_tiles = l.score_tiles;
         p.n = l.n;
         std::memcpy(p.rows, l.rows, l.n * sizeof(SelectRow));
         return launch_select(p, cache->head_dim, l.groups, l.score_blocks, l.max_keys, static_cast<hipStream_t>(stream)) == hipSuccess ? AMPD_OK : AMPD_ERR_HIP;
-    });
+    };
+    return plan.launches == 1 ? launch(plan.only) : select_launches(cache, batch, sel, launch);
 }
 
 ampd_status ampd_sparse_attn(const ampd_kv_cache* cache, const ampd_batch* batch, const int32_t* selected, int32_t budget, int32_t group_tokens,
@@ -145,7 +148,9 @@ ampd_status ampd_sparse_attn(const ampd_kv_cache* cache, const ampd_batch* batch
     if ((vs = validate_sparse(cache, batch, budget, group_tokens)) != AMPD_OK) return vs;
     if (nothing_new(batch)) return AMPD_OK;
     if (!aligned(selected, 4) || !aligned(q, 16) || !aligned(out, 16)) return AMPD_ERR_INVALID_ARG;
-    if (!aligned(workspace, 256) || workspace_bytes < ampd_sparse_attn_workspace_bytes(cache, batch, budget, group_tokens)) return AMPD_ERR_WORKSPACE;
+    SparsePlan plan;
+    sparse_plan(cache, batch, budget, group_tokens, &plan);
+    if (!aligned(workspace, 256) || workspace_bytes < (size_t)plan.bytes) return AMPD_ERR_WORKSPACE;
     SparseParams p;
     p.q = q;
     p.out = out;
@@ -164,7 +169,7 @@ ampd_status ampd_sparse_attn(const ampd_kv_cache* cache, const ampd_batch* batch
     p.budget = budget;
     p.g = group_tokens;
     p.c_log2 = cache->softmax_scale * 1.44269504088896340736f;
-    return sparse_launches(cache, batch, budget, group_tokens, [&](const SparseLaunch& l) {
+    auto launch = [&](const SparseLaunch& l) {
         p.selected = selected + l.group0 * cache->num_kv_heads * budget;
         p.tiles = l.tiles;
         p.splits = l.splits;
@@ -172,7 +177,8 @@ ampd_status ampd_sparse_attn(const ampd_kv_cache* cache, const ampd_batch* batch
         p.n = l.n;
         std::memcpy(p.rows, l.rows, l.n * sizeof(SparseRow));
         return launch_sparse(p, cache->head_dim, kv_type(cache), l.groups, l.waves, static_cast<hipStream_t>(stream)) == hipSuccess ? AMPD_OK : AMPD_ERR_HIP;
-    });
+    };
+    return plan.launches == 1 ? launch(plan.only) : sparse_launches(cache, batch, budget, group_tokens, launch);
 }
 
 }  // extern "C"

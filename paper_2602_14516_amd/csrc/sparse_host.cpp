@@ -121,13 +121,26 @@ ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const a
     return st;
 }
 
-int64_t select_keys_bytes(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* s) {
-    int64_t most = 0;
+void select_plan(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* s, SelectPlan* out) {
+    int64_t groups = 0;
     select_launches(c, b, s, [&](const SelectLaunch& l) {
-        most = std::max(most, l.keys * 4);
+        out->keys_bytes = std::max(out->keys_bytes, l.keys * 4);
+        groups = std::max(groups, (int64_t)l.groups);
+        if (out->launches++ == 0) out->only = l;
         return AMPD_OK;
     });
-    return (most + 255) / 256 * 256;
+    out->keys_bytes = (out->keys_bytes + 255) / 256 * 256;
+    out->bytes = std::max<int64_t>(256, out->keys_bytes + groups * c->num_kv_heads * 4 * c->head_dim);
+}
+
+void sparse_plan(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, int32_t g, SparsePlan* out) {
+    int64_t floats = 0;
+    sparse_launches(c, b, budget, g, [&](const SparseLaunch& l) {
+        floats = std::max(floats, l.partial_floats);
+        if (out->launches++ == 0) out->only = l;
+        return AMPD_OK;
+    });
+    out->bytes = std::max<int64_t>(256, floats * 4);
 }
 
 ampd_status sparse_launches(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, int32_t g, LaunchFn<SparseLaunch> f) {
@@ -189,22 +202,16 @@ extern "C" {
 
 size_t ampd_select_pages_workspace_bytes(const ampd_kv_cache* cache, const ampd_batch* batch, const ampd_page_selection* sel) {
     if (validate_select(cache, batch, sel) != AMPD_OK) return 0;
-    int64_t groups = 0;
-    select_launches(cache, batch, sel, [&](const SelectLaunch& l) {
-        groups = std::max(groups, (int64_t)l.groups);
-        return AMPD_OK;
-    });
-    return (size_t)std::max<int64_t>(256, select_keys_bytes(cache, batch, sel) + groups * cache->num_kv_heads * 4 * cache->head_dim);
+    SelectPlan plan;
+    select_plan(cache, batch, sel, &plan);
+    return (size_t)plan.bytes;
 }
 
 size_t ampd_sparse_attn_workspace_bytes(const ampd_kv_cache* cache, const ampd_batch* batch, int32_t budget, int32_t group_tokens) {
     if (validate_sparse(cache, batch, budget, group_tokens) != AMPD_OK) return 0;
-    int64_t floats = 0;
-    sparse_launches(cache, batch, budget, group_tokens, [&](const SparseLaunch& l) {
-        floats = std::max(floats, l.partial_floats);
-        return AMPD_OK;
-    });
-    return (size_t)std::max<int64_t>(256, floats * 4);
+    SparsePlan plan;
+    sparse_plan(cache, batch, budget, group_tokens, &plan);
+    return (size_t)plan.bytes;
 }
 
 }  // extern "C"
