@@ -1220,6 +1220,8 @@ __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparsePar
             st.l += exp_sum<8>(p.c_log2, st.m == NEG_INF ? 0.0f : st.m, false, [&](int i) { return S[i >> 2][i & 3]; }, [&](int i, __bf16 v) { P[i] = v; });
             pv16<D>(vl, P, st, lane);
         } else {
+            // a wave that has begun a block's products goes first: 64 groups of 32 rows over 128 pages 42.0 -> 40.4 us (LDS is what it waits for)
+            __builtin_amdgcn_s_setprio(1);
             f32x16 S;
             bf16x8 P[2];
             qk32<D>(kl, Q, S, lane);
@@ -1234,6 +1236,7 @@ __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparsePar
             if (__any(mx > st.m + RESCALE_SLACK)) raise_reference<D>(st, mx);
             st.l += exp_sum<16>(p.c_log2, st.m == NEG_INF ? 0.0f : st.m, false, [&](int i) { return S[i]; }, [&](int i, __bf16 v) { P[i >> 3][i & 7] = v; });
             pv32<D>(vl, P, st, lane);
+            __builtin_amdgcn_s_setprio(0);
         }
     }
     // merge the waves' states: LDS holds O as [state][row][D + 4] fp32 and (m, l) as [state][row][2]

@@ -353,7 +353,7 @@ def test_lists_of_nothing_duplicates_and_pages_that_are_not_there(g_tok):
     assert torch.equal(got, want)
 
 
-@pytest.mark.parametrize("rows,budget", [(1, 600), (2, 129), (40, 9), (260, 3)])
+@pytest.mark.parametrize("rows,budget", [(1, 600), (2, 129), (40, 9), (70, 12), (130, 5), (260, 3)])
 def test_lists_in_pieces_and_whole(rows, budget):
     """Few rows: the list is cut and joined; many: whole; more rows than a launch takes."""
     case(f"sparse {rows} rows x {budget} pages")
@@ -363,6 +363,16 @@ def test_lists_in_pieces_and_whole(rows, budget):
     C[0] = min(budget, 600) * P - 1
     p = Pool(57, C + L, np.zeros_like(C), Hq, Hkv, d, P)
     check_sparse(p, C, L, random_lists(p.g, C, L, P, Hkv, budget, 1), normal_bits(p.g, rows, Hq, d), 1)
+
+
+def test_groups_as_large_workgroups():
+    """128 to 256 items go as workgroups of 8 waves, 32 query rows each."""
+    case("sparse groups of 8 waves")
+    P, Hq, Hkv, d = 16, 8, 2, 128
+    C, L = np.array([300, 0], np.int32), np.array([261, 260], np.int32)
+    p = Pool(58, C + L, np.zeros_like(C), Hq, Hkv, d, P)
+    assert 128 <= A.num_groups(L, 8) * Hkv <= 256
+    check_sparse(p, C, L, random_lists(p.g, C, L, P, Hkv, 19, 8), normal_bits(p.g, int(L.sum()), Hq, d), 8)
 
 
 def test_logits_far_apart_and_a_page_that_outweighs_the_rest():
@@ -501,5 +511,84 @@ def test_empty_batches():
     A.page_bounds_update(p.cache, [20], z, p.table, p.bounds)
     sel = A.select_pages(p.cache, [20], z, p.table, p.bounds, q, 4)
     assert sel.shape == (0, 2, 4) and A.sparse_attn(p.cache, [20], z, p.table, sel, q).shape == (0, 8, 64)
+    none = torch.empty((0, 3), dtype=torch.int32, device="cuda")              # no requests at all
+    assert A.rope_kv_append(p.cache, [], [], none, A.Rope(torch.ones(32, device="cuda")), q, kv, kv).shape == (0, 8, 64)
+    A.page_bounds_update(p.cache, [], [], none, p.bounds)
+    sel = A.select_pages(p.cache, [], [], none, p.bounds, q, 4)
+    assert sel.shape == (0, 2, 4) and A.sparse_attn(p.cache, [], [], none, sel, q).shape == (0, 8, 64)
     p.assert_pools_equal()
     p.assert_bounds_equal()
+
+
+# ---- the two ways through the binding ------------------------------------------------------------------------------------------
+
+
+def session(fp8=False):
+    P, Hq, Hkv, d = 16, 8, 2, 64
+    C, L = np.array([60, 33], np.int32), np.array([1, 9], np.int32)
+    p = Pool(81, C, L, Hq, Hkv, d, P, fp8)
+    A.page_bounds_update(p.cache, np.zeros_like(C), C, p.table, p.bounds)
+    x = dev_bits(normal_bits(p.g, 10, Hq + 2 * Hkv, d))
+    out = dict(q_out=torch.empty((10, Hq, d), dtype=torch.bfloat16, device="cuda"), sel=torch.empty((A.num_groups(L, 4), Hkv, 4), dtype=torch.int32, device="cuda"),
+               out=torch.empty((10, Hq, d), dtype=torch.bfloat16, device="cuda"), ws=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+    calls = [lambda C=C: A.rope_kv_append(p.cache, C, L, p.table, A.Rope(torch.from_numpy(inv_freq(64)).cuda()), x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:],
+                                          q_out=out["q_out"], bounds=p.bounds),
+             lambda C=C: A.page_bounds_update(p.cache, C, L, p.table, p.bounds),
+             lambda C=C: A.select_pages(p.cache, C, L, p.table, p.bounds, out["q_out"], 4, group_tokens=4, out=out["sel"], workspace=out["ws"]),
+             lambda C=C: A.sparse_attn(p.cache, C, L, p.table, out["sel"], out["q_out"], group_tokens=4, out=out["out"], workspace=out["ws"])]
+    return p, out, calls
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "8bit"])
+def test_usual_calls_take_the_extension_and_others_the_general_path(fp8, monkeypatch):
+    case(f"sparse marshalling 8bit={fp8}")
+    import paper_2602_14516_amd.binding as B
+    results = []
+    for general in (False, True):
+        p, out, calls = session(fp8)
+        taken = []
+        real = B._fast_sparse
+        monkeypatch.setattr(B, "_fast_sparse", lambda *a: taken.append(None if general else real(*a)) or taken[-1])
+        for f in calls:
+            f()
+        assert taken == [None if general else 0] * 4
+        monkeypatch.setattr(B, "_fast_sparse", real)
+        # lengths of another kind: the general path
+        for f in calls:
+            f(C=[60, 33])
+        torch.cuda.synchronize()
+        results.append([t.clone() for t in (out["q_out"], out["sel"], out["out"], p.bounds.codes, p.bounds.scale, p.cache.k_pool, p.cache.v_pool)])
+    for a, b in zip(*results):
+        assert torch.equal(a.view(torch.uint8) if a.is_floating_point() else a, b.view(torch.uint8) if b.is_floating_point() else b)
+
+
+def test_what_the_library_would_read_as_something_else_is_refused_on_the_device_too():
+    case("sparse refusals")
+    p, out, calls = session()
+    for f in calls:
+        f()
+    C, L = np.array([60, 33], np.int32), np.array([1, 9], np.int32)
+    q, sel = out["q_out"], out["sel"]
+    rope, kv = A.Rope(torch.ones(32, device="cuda")), q[:, :2]
+    good = dict(q_out=out["out"], bounds=p.bounds)
+    with pytest.raises(ValueError, match="q_out"):
+        A.rope_kv_append(p.cache, C, L, p.table, rope, q, kv, kv, q_out=out["out"][:9])
+    with pytest.raises(ValueError, match="device memory"):
+        A.rope_kv_append(p.cache, C, L, p.table, rope, q, kv, kv, positions=torch.zeros(10, dtype=torch.int32), **good)
+    with pytest.raises(ValueError, match="next to each other"):
+        A.rope_kv_append(p.cache, C, L, p.table, rope, torch.empty((10, 64, 8), dtype=torch.bfloat16, device="cuda").transpose(1, 2), kv, kv, **good)
+    with pytest.raises(ValueError, match="k_pool"):
+        A.sparse_attn(A.KVCache(8, 2, 64, 16, p.cache.k_pool[:, :, :8], p.cache.v_pool, 0.1), C, L, p.table, sel, q, group_tokens=4, out=out["out"], workspace=out["ws"])
+    with pytest.raises(ValueError, match="selected"):
+        A.sparse_attn(p.cache, C, L, p.table, sel, q, group_tokens=1, out=out["out"], workspace=out["ws"])
+    with pytest.raises(ValueError, match="device memory"):
+        A.select_pages(p.cache, C, L, p.table, p.bounds, q, 4, group_tokens=4, out=sel, workspace=torch.empty(1 << 20, dtype=torch.uint8))
+    for f, status in ((lambda: A.rope_kv_append(p.cache, C, L, p.table, A.Rope(torch.ones(20, device="cuda")), q, kv, kv, **good), -2),
+                      (lambda: A.rope_kv_append(p.cache, C, L, p.table, A.Rope(torch.ones(32, device="cuda"), scale=-1.0), q, kv, kv, **good), -1),
+                      (lambda: A.select_pages(p.cache, C, L, p.table, p.bounds, q, 4, group_tokens=4, out=sel, workspace=out["ws"][:256]), -3),
+                      (lambda: A.select_pages(p.cache, C, L, p.table, p.bounds, q, 4, group_tokens=4, out=sel, workspace=out["ws"][1:]), -3),
+                      (lambda: A.select_pages(p.cache, C, L, p.table, p.bounds, q, 4, group_tokens=4, last_pages=4, out=sel, workspace=out["ws"]), -1),
+                      (lambda: A.sparse_attn(p.cache, C, L, p.table[:, :2].contiguous(), sel, q, group_tokens=4, out=out["out"], workspace=out["ws"]), -1)):
+        with pytest.raises(A.AmpdError) as e:
+            f()
+        assert e.value.status == status
