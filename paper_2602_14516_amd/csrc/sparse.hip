@@ -427,7 +427,8 @@ __global__ __launch_bounds__(WG) void rope_append_kernel(const RopeParams p) {
 // page selection
 
 // The row of a launch that owns item idx: the last one that starts at or before it.  Every lane loads a row or two and the owner's is picked
-// from the lanes: one trip to the arguments.
+// from the lanes.  The loads do not wait for n, so they make one trip to the arguments together with the scalar ones (what lies behind the n rows
+// is not looked at).
 template <int MAX, class Row, class F>
 __device__ __forceinline__ Row row_of(const Row* rows, int n, int idx, F&& start) {
     static_assert(MAX > 64 && MAX <= 128 && sizeof(Row) % 4 == 0, "two rows per lane");
@@ -436,9 +437,7 @@ __device__ __forceinline__ Row row_of(const Row* rows, int n, int idx, F&& start
         int32_t w[W];
     };
     const int lane = threadIdx.x & 63;
-    const Row a = rows[min(lane, n - 1)];
-    Row b = a;
-    if (n > 64) b = rows[min(lane + 64, n - 1)];
+    const Row a = rows[lane], b = rows[min(lane + 64, MAX - 1)];
     const int r = __popcll(__ballot(lane < n && start(a) <= idx)) + __popcll(__ballot(lane + 64 < n && start(b) <= idx)) - 1;
     const Words x = __builtin_bit_cast(Words, a), y = __builtin_bit_cast(Words, b);
     Words out;
@@ -1039,14 +1038,13 @@ struct ListLoader {
     float scale[4], sc[4];
     static constexpr int NONE = 0x3fffffff;
 
-    __device__ __forceinline__ void fetch_entries(const SparseParams& p, const int32_t* list, int last_page, int key0, int step, int end, int j, int lane) {
+    __device__ __forceinline__ void fetch_entries(const SparseParams& p, const int32_t* list, int key0, int step, int end, int j, int lane) {
         const int pos = key0 + (j + (lane >> 1) % IDS) * step + (lane & 1) * 16;
-        int e = -1;
-        if (pos < end) e = list[pos >> p.logP];
-        next = e <= last_page ? e : -1;
+        next = -1;
+        if (pos < end) next = list[pos >> p.logP];
     }
-    __device__ __forceinline__ void fetch_pages(const SparseParams& p, const int32_t* bt) {
-        entry = next;
+    __device__ __forceinline__ void fetch_pages(const SparseParams& p, const int32_t* bt, int last_page) {
+        entry = next <= last_page ? next : -1;
         int id = -1;
         if (entry >= 0) id = bt[entry];
         page = (uint32_t)id < (uint64_t)p.num_pages ? id : -1;
@@ -1111,26 +1109,29 @@ struct ListLoader {
 struct SparseItem {
     int kvh, G, rows;                                 // rows of this tile: row r is row r0 + r of the group, token / G
     int r0, tok0, C, row_off;
-    int piece, linear;
-    int64_t group;                                    // of the launch
+    int piece, tile, linear;
+    int group;                                        // of the launch
     int req;
 };
-__device__ __forceinline__ bool sparse_item(const SparseParams& p, int ROWS, int b, SparseItem& it) {
+// Workgroups in launch order: KV head first (neighbouring workgroups run on different dies; a head's groups share lines on one die where the heads
+// are as many), then piece, row tile, group.
+__device__ __forceinline__ void sparse_place(const SparseParams& p, int b, SparseItem& it) {
     it.linear = b;
     it.kvh = b % p.Hkv;
     b /= p.Hkv;
     it.piece = b % p.splits;
     b /= p.splits;
-    const int tile = b % p.tiles;
-    b /= p.tiles;
-    it.group = b;
-    const SparseRow r = row_of<SPARSE_MAX_REQS>(p.rows, p.n, b, [](const SparseRow& x) { return x.first; });
+    it.tile = b % p.tiles;
+    it.group = b / p.tiles;
+}
+__device__ __forceinline__ bool sparse_item(const SparseParams& p, int ROWS, SparseItem& it) {
+    const SparseRow r = row_of<SPARSE_MAX_REQS>(p.rows, p.n, it.group, [](const SparseRow& x) { return x.first; });
     it.req = r.req;
     it.G = p.Hq / p.Hkv;
-    it.tok0 = (b - r.first) * p.g;
+    it.tok0 = (it.group - r.first) * p.g;
     it.C = r.C;
     it.row_off = r.row_off;
-    it.r0 = tile * ROWS;
+    it.r0 = it.tile * ROWS;
     it.rows = min(ROWS, min(p.g, r.L - it.tok0) * it.G - it.r0);
     return it.rows > 0;
 }
@@ -1150,22 +1151,23 @@ __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparsePar
     __shared__ __attribute__((aligned(16))) char smem_raw[sparse_smem<D, NW, ROWS>()];
     const uint32_t smem = (uint32_t)(uintptr_t)LDS_PTR(char, smem_raw);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // (the first list entries before the row they belong to is known)
     SparseItem it;
-    if (!sparse_item(p, ROWS, blockIdx.x, it)) return;
+    sparse_place(p, blockIdx.x, it);
+    const int begin = it.piece * p.chunk, end = min(p.budget << p.logP, begin + p.chunk);
+    const int nblocks = (end - begin + 31) >> 5, step = 32 * NW, key0 = begin + wave * 32;
+    const int nj = (nblocks - wave + NW - 1) / NW;
+    const int32_t* list = p.selected + ((int64_t)it.group * p.Hkv + it.kvh) * p.budget;
+    ListLoader<D, KVT, ONCE> ld;
+    if (nj > 0) ld.fetch_entries(p, list, key0, step, end, 0, lane);
+    if (!sparse_item(p, ROWS, it)) return;
     const int row = lane & (ROWS - 1);
     const bool valid = row < it.rows;
     const int gr = it.r0 + min(row, it.rows - 1), tok = it.tok0 + gr / it.G;
     const int lim = it.C + tok;                                           // last visible position
     const int first_lim = it.C + it.tok0 + it.r0 / it.G, last_lim = it.C + it.tok0 + (it.r0 + it.rows - 1) / it.G;
     const int last_page = last_lim >> p.logP;
-    const int begin = it.piece * p.chunk, end = min(p.budget << p.logP, begin + p.chunk);
-    const int nblocks = (end - begin + 31) >> 5, step = 32 * NW, key0 = begin + wave * 32;
-    const int nj = (nblocks - wave + NW - 1) / NW;
-    const int32_t* list = p.selected + (it.group * p.Hkv + it.kvh) * p.budget;
     const int32_t* bt = p.block_table + (int64_t)it.req * p.max_pages;
-
-    ListLoader<D, KVT, ONCE> ld;
-    if (nj > 0) ld.fetch_entries(p, list, last_page, key0, step, end, 0, lane);
     bf16x8 Q[R16 ? D / 32 : G_::NKK];
     {
         const int hq = it.kvh * it.G + gr % it.G, g = lane / ROWS;
@@ -1188,16 +1190,16 @@ __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparsePar
     const uint32_t kl = smem + wave * (2 * G_::B32), vl = kl + G_::B32;
     bool have = false;
     if (nj > 0) {
-        ld.fetch_pages(p, bt);
+        ld.fetch_pages(p, bt, last_page);
         have = ld.fetch(p, it.kvh, key0, 0, lane);
     }
     for (int j = 0; j < nj; ++j) {
         const bool now = have;                                            // uniform
         if (now) ld.commit(kl, vl, last_lim, lane);
         if (j + 1 < nj) {
-            if ((j + 1) % ld.IDS == 0) ld.fetch_pages(p, bt);
+            if ((j + 1) % ld.IDS == 0) ld.fetch_pages(p, bt, last_page);
             have = ld.fetch(p, it.kvh, key0 + (j + 1) * step, j + 1, lane);
-            if ((j + 1) % ld.IDS == ld.IDS - 1) ld.fetch_entries(p, list, last_page, key0, step, end, j + 2, lane);
+            if ((j + 1) % ld.IDS == ld.IDS - 1) ld.fetch_entries(p, list, key0, step, end, j + 2, lane);
         }
         if (!now) continue;
         const bool masked = max(ld.at[0], ld.at[1]) + 15 > first_lim;
@@ -1316,23 +1318,22 @@ __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparsePar
     }
 }
 
-// Merge the pieces of a list: one workgroup per (group, row tile, KV head) and pass of WG / (D / 4) rows.
+// Merge the pieces of a list: one workgroup per (group, row tile, KV head) and pass of WG / (D / 4) rows.  Up to UN pieces are on their way before
+// the row they belong to is known (rows that a tile does not have are read too, and dropped).
 template <int D, int ROWS>
 __global__ __launch_bounds__(WG) void sparse_join_kernel(const SparseParams p) {
-    constexpr int QPR = D / 4, RPP = WG / QPR;
+    constexpr int QPR = D / 4, RPP = WG / QPR, UN = 16;
     SparseItem it;
     const int b = blockIdx.x, kvh = b % p.Hkv;
-    if (!sparse_item(p, ROWS, (b / p.Hkv) * p.splits * p.Hkv + kvh, it)) return;
+    sparse_place(p, (b / p.Hkv) * p.splits * p.Hkv + kvh, it);
     const int r = blockIdx.y * RPP + threadIdx.x / QPR, dq = (threadIdx.x % QPR) * 4;
-    if (r >= it.rows) return;
     const int64_t stride = (int64_t)p.Hkv * (ROWS * (D + 2));             // from piece to piece
     const float* base = p.partial + (int64_t)it.linear * (ROWS * (D + 2));
     float m = NEG_INF, l = 0.0f;
     f32x4 acc = {0, 0, 0, 0};
-    constexpr int UN = 16;                            // (all of them, as a rule)
-    for (int s0 = 0; s0 < p.splits; s0 += UN) {
-        float mv[UN], lv[UN];
-        f32x4 ov[UN];
+    float mv[UN], lv[UN];
+    f32x4 ov[UN];
+    auto fetch = [&](int s0) {
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
             const float* part = base + min(s0 + i, p.splits - 1) * stride;
@@ -1340,6 +1341,11 @@ __global__ __launch_bounds__(WG) void sparse_join_kernel(const SparseParams p) {
             lv[i] = part[ROWS * D + r * 2 + 1];
             ov[i] = *reinterpret_cast<const f32x4*>(part + r * D + dq);
         }
+    };
+    fetch(0);
+    const bool there = sparse_item(p, ROWS, it) && r < it.rows;
+    for (int s0 = 0; s0 < p.splits; s0 += UN) {
+        if (s0 > 0) fetch(s0);
         float mg = m;
 #pragma unroll
         for (int i = 0; i < UN; ++i) mg = fmaxf(mg, mv[i]);
@@ -1356,6 +1362,7 @@ __global__ __launch_bounds__(WG) void sparse_join_kernel(const SparseParams p) {
         }
         m = mg;
     }
+    if (!there) return;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     const int t = (it.r0 + r) / it.G, hq = it.kvh * it.G + (it.r0 + r) - t * it.G;
     char* dst = static_cast<char*>(p.out) + (((int64_t)(it.row_off + it.tok0 + t) * p.Hq + hq) * D + dq) * 2;
