@@ -545,7 +545,7 @@ def _rows(name, t, tokens, heads, d):
     s = t.stride()
     if tokens and (s[2] != 1 or heads > 1 and s[1] != d):
         raise ValueError(f"{name}: the heads of a token have to lie next to each other (strides {tuple(s)})")
-    return max(int(s[0]), heads * d) if tokens < 2 else int(s[0])
+    return int(s[0]) if tokens > 1 else heads * d
 
 
 def _lengths(ctx_len, incr_len):

@@ -6,7 +6,6 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
-#include <algorithm>
 #include <cfloat>
 #include <climits>
 #include <cmath>
@@ -226,7 +225,7 @@ struct SparseCall : Call {
             t->size(2) != c.head_dim || tokens < 1 || t->stride(2) != 1 || (heads > 1 && t->stride(1) != c.head_dim))
             return false;
         *p = t->data_ptr();
-        *stride = tokens < 2 ? std::max(t->stride(0), heads * c.head_dim) : t->stride(0);
+        *stride = tokens > 1 ? t->stride(0) : heads * c.head_dim;
         return true;
     }
     bool bounds(PyObject* o, ampd_page_bounds* b) const {
