@@ -1150,7 +1150,7 @@ constexpr int sparse_smem() {
 // matrix cores take in 16 bits (their sum is taken before).
 // Bound: memory where every list is another's (96 rows x 8 heads over 128 pages of 16, 809 MB in 130 us = 6.2 TB/s); LDS, through which K and V
 // pass on their way into the operands' layout, where 32 rows share a list that is in L2 (64 groups: 40 us, on pages that never leave L2 38; K loaded
-// straight in the operand's layout, half lines at a time, 52).
+// straight in the layout of a 32x32x16 or two 16x16x32 products, quarter or half lines at a time, 52 and 50).
 template <int D, int KVT, int ROWS, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparseParams p) {
     using G_ = Geo<D>;
