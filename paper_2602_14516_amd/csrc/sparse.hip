@@ -38,41 +38,84 @@ __device__ __forceinline__ void decode8(uint32_t lo, uint32_t hi, float (&f)[8])
     f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
 }
 
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
-    return x;
+template <int CTRL>
+__device__ __forceinline__ uint32_t add_dpp(uint32_t x) {
+    return x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+// the sum over the 16 lanes of a row, in all of them
+__device__ __forceinline__ uint32_t row_sum(uint32_t x) {
+    x = add_dpp<0xB1>(x);                             // quad_perm [1, 0, 3, 2]
+    x = add_dpp<0x4E>(x);                             // quad_perm [2, 3, 0, 1]
+    x = add_dpp<0x124>(x);                            // row_ror:4
+    return add_dpp<0x128>(x);                         // row_ror:8
 }
 
-// The lane's largest and smallest values so far of its 16 channels (chunk a: 0..7, chunk b: 8..15), over its own units.
+__device__ __forceinline__ uint32_t max16x2(uint32_t a, uint32_t b) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
+    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
+    x = max_dpp<0xB1>(x);
+    x = max_dpp<0x4E>(x);
+    x = max_dpp<0x124>(x);
+    x = max_dpp<0x128>(x);
+    u32x2 r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max(r[0], r[1]);
+}
+__device__ __forceinline__ uint32_t wave_umin(uint32_t x) { return ~wave_umax(~x); }
+__device__ __forceinline__ uint32_t wave_usum(uint32_t x) {
+    x = row_sum(x);
+    u32x2 r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = r[0] + r[1];
+    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return r[0] + r[1];
+}
+
+// the largest of non-negative numbers
+__device__ __forceinline__ float wave_max(float x) { return __uint_as_float(wave_umax(__float_as_uint(x))); }
+
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t smax16x2(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
+}
+__device__ __forceinline__ uint32_t smin16x2(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
+}
+// Two bf16 values as whole numbers that order as they do, and back: the magnitude of negative ones is inverted.
+__device__ __forceinline__ uint32_t ordered16x2(uint32_t x) {
+    const i16x2 sign = __builtin_bit_cast(i16x2, x) >> 15;
+    return x ^ (__builtin_bit_cast(uint32_t, sign) & 0x7fff7fffu);
+}
+
+// The lane's largest and smallest values so far of its 16 channels (chunk a: words 0..3, chunk b: 4..7, two channels each), over its own units.
+// (Two to an instruction, and exchanged by swaps of lanes: in 32 bits with exchanges through LDS a reply of 701 tokens took 3.8 us instead of 3.1,
+// one token rotated and appended 5.7 instead of 5.0.)
 struct LaneBounds {
-    float hi[16], lo[16];
+    uint32_t hi[8], lo[8];
     __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            hi[i] = NEG_INF;
-            lo[i] = -NEG_INF;
-        }
-    }
-    __device__ __forceinline__ void take(int at, const float (&f)[8]) {
-#pragma unroll
         for (int i = 0; i < 8; ++i) {
-            hi[at + i] = fmaxf(hi[at + i], f[i]);
-            lo[at + i] = fminf(lo[at + i], f[i]);
+            hi[i] = 0x80008000u;
+            lo[i] = 0x7fff7fffu;
         }
     }
-};
-
-// Half of the N values that the lane holds go to the lane `bit` away, which sends the other half: what stays is over both lanes.
-template <int N>
-__device__ __forceinline__ void exchange(float (&hi)[16], float (&lo)[16], int bit, bool upper) {
+    __device__ __forceinline__ void take(int at, const u32x4& chunk) {
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-        const float h = __shfl_xor(upper ? hi[i] : hi[N / 2 + i], bit, 64), l = __shfl_xor(upper ? lo[i] : lo[N / 2 + i], bit, 64);
-        hi[i] = fmaxf(upper ? hi[N / 2 + i] : hi[i], h);
-        lo[i] = fminf(upper ? lo[N / 2 + i] : lo[i], l);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = ordered16x2(chunk[i]);
+            hi[at + i] = smax16x2(hi[at + i], x);
+            lo[at + i] = smin16x2(lo[at + i], x);
+        }
     }
-}
+    // 8-bit codes as their values
+    __device__ __forceinline__ void take_codes(int at, uint32_t c0, uint32_t c1) { take(at, RawChunk<KV_FP8>::widen8(c0, c1, 1.0f)); }
+};
 
 // smallest e with amax <= 127 * 2^e  (127 = 1.984375 * 2^6), clamped to [-40, 96]
 __device__ __forceinline__ int bounds_exponent(float amax) {
@@ -84,46 +127,57 @@ __device__ __forceinline__ int bounds_exponent(float amax) {
 }
 
 // Bounds of a page of one KV head from the wave's lanes; unit: what the lanes' values count in (a power of two: an 8-bit page's scale).
-// The lanes that share a pair of chunks halve their values log2(64 / (D / 16)) times, so that 28 exchanges do instead of 96.
+// The 64 / (D / 16) lanes that share a pair of chunks halve their words three times: a swap of rows of lanes leaves each lane both lanes' values
+// of the half that it keeps.
 template <int D>
 __device__ __forceinline__ void store_bounds(LaneBounds& b, float unit, int ca, int cb, int lane, int8_t* codes, float* scale) {
-    exchange<16>(b.hi, b.lo, 32, lane & 32);
-    exchange<8>(b.hi, b.lo, 16, lane & 16);
-    exchange<4>(b.hi, b.lo, 8, lane & 8);
-    if constexpr (D == 64) exchange<2>(b.hi, b.lo, 4, lane & 4);
-    constexpr int N = D == 64 ? 1 : 2;                // neighbouring channels that the lane is left with
-    const int x = (lane & 32 ? cb : ca) * 8 + (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0) + (D == 64 && (lane & 4) ? 1 : 0);
-    float amax = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        b.hi[i] *= unit;
-        b.lo[i] *= unit;
-        amax = fmaxf(amax, fmaxf(fabsf(b.hi[i]), fabsf(b.lo[i])));
+    for (int i = 0; i < 4; ++i) {                     // lanes 0..31 keep chunk a
+        const u32x2 h = __builtin_amdgcn_permlane32_swap(b.hi[i], b.hi[4 + i], false, false), l = __builtin_amdgcn_permlane32_swap(b.lo[i], b.lo[4 + i], false, false);
+        b.hi[i] = smax16x2(h[0], h[1]);
+        b.lo[i] = smin16x2(l[0], l[1]);
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                     // rows 0 and 2 of 16 lanes words 0 and 1
+        const u32x2 h = __builtin_amdgcn_permlane16_swap(b.hi[i], b.hi[2 + i], false, false), l = __builtin_amdgcn_permlane16_swap(b.lo[i], b.lo[2 + i], false, false);
+        b.hi[i] = smax16x2(h[0], h[1]);
+        b.lo[i] = smin16x2(l[0], l[1]);
+    }
+    const bool upper = lane & 8;                      // lanes 0..7 of a row the first of the two
+    auto other = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true); };     // row_ror:8
+    uint32_t hw = smax16x2(upper ? b.hi[1] : b.hi[0], other(upper ? b.hi[0] : b.hi[1]));
+    uint32_t lw = smin16x2(upper ? b.lo[1] : b.lo[0], other(upper ? b.lo[0] : b.lo[1]));
+    if constexpr (D == 64) {                          // four pairs to a key: lanes 4 apart share one still
+        hw = smax16x2(hw, (uint32_t)__shfl_xor((int)hw, 4, 64));
+        lw = smin16x2(lw, (uint32_t)__shfl_xor((int)lw, 4, 64));
+    }
+    hw = ordered16x2(hw);
+    lw = ordered16x2(lw);
+    const int x = (lane & 32 ? cb : ca) * 8 + (lane & 16 ? 4 : 0) + (upper ? 2 : 0);     // the first of the lane's two channels
+    const float hv[2] = {__uint_as_float(hw << 16) * unit, __uint_as_float(hw & 0xffff0000u) * unit};
+    const float lv[2] = {__uint_as_float(lw << 16) * unit, __uint_as_float(lw & 0xffff0000u) * unit};
+    const float amax = fmaxf(fmaxf(fabsf(hv[0]), fabsf(hv[1])), fmaxf(fabsf(lv[0]), fabsf(lv[1])));
     const int e = bounds_exponent(wave_max(amax));
     const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-    int8_t h[N], l[N];
+    uint32_t h = 0, l = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < 2; ++i) {
         // (a value that underflows when it is scaled still counts)
-        float u = ceilf(b.hi[i] * inv), d = floorf(b.lo[i] * inv);
-        if (b.hi[i] > 0.0f) u = fmaxf(u, 1.0f);
-        if (b.lo[i] < 0.0f) d = fminf(d, -1.0f);
-        h[i] = (int8_t)(int)fminf(fmaxf(u, -127.0f), 127.0f);
-        l[i] = (int8_t)(int)fminf(fmaxf(d, -127.0f), 127.0f);
+        float u = ceilf(hv[i] * inv), d = floorf(lv[i] * inv);
+        if (hv[i] > 0.0f) u = fmaxf(u, 1.0f);
+        if (lv[i] < 0.0f) d = fminf(d, -1.0f);
+        h |= ((uint32_t)(int)fminf(fmaxf(u, -127.0f), 127.0f) & 0xff) << (8 * i);
+        l |= ((uint32_t)(int)fminf(fmaxf(d, -127.0f), 127.0f) & 0xff) << (8 * i);
     }
-    if constexpr (N == 2) {
-        *reinterpret_cast<uint16_t*>(codes + x) = (uint16_t)((uint8_t)h[0] | (uint8_t)h[1] << 8);
-        *reinterpret_cast<uint16_t*>(codes + D + x) = (uint16_t)((uint8_t)l[0] | (uint8_t)l[1] << 8);
-    } else {
-        codes[x] = h[0];
-        codes[D + x] = l[0];
+    if (D == 128 || !(lane & 4)) {
+        *reinterpret_cast<uint16_t*>(codes + x) = (uint16_t)h;
+        *reinterpret_cast<uint16_t*>(codes + D + x) = (uint16_t)l;
     }
     if (lane == 0) *scale = __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
-// A wave per page and KV head.  Non-temporal loads: 165 MB 31.5 us instead of 35.2.  (Two heads per wave 30.6 us, but a reply of 701 tokens 4.7
-// instead of 3.8.)
+// A wave per page and KV head.  Bound: memory, 165 MB in 31 us (35 without non-temporal loads), of which the launch's beginning and end are 4.
+// (Two heads per wave gain 3 % of that, and cost a reply of 701 tokens 25 %.)
 template <int D, int P, int KVT>
 __global__ __launch_bounds__(WG) void page_bounds_kernel(const BoundsParams p) {
     constexpr int PPT = Units<D>::PPT, NU = Units<D>::COUNT(P);
@@ -150,17 +204,12 @@ __global__ __launch_bounds__(WG) void page_bounds_kernel(const BoundsParams p) {
     }
 #pragma unroll
     for (int k = 0; k < NU; ++k) {
-        float f[8];
         if constexpr (KVT == KV_BF16) {
-            unpack8(x[k], f);
-            b.take(0, f);
-            unpack8(y[k], f);
-            b.take(8, f);
+            b.take(0, x[k]);
+            b.take(4, y[k]);
         } else {
-            decode8(x[k].x, x[k].y, f);
-            b.take(0, f);
-            decode8(x[k].z, x[k].w, f);
-            b.take(8, f);
+            b.take_codes(0, x[k].x, x[k].y);
+            b.take_codes(4, x[k].z, x[k].w);
         }
     }
     const int ca = KVT == KV_BF16 ? pair : 2 * pair, cb = KVT == KV_BF16 ? pair + PPT : 2 * pair + 1;
@@ -237,7 +286,7 @@ __device__ __forceinline__ void rotate(u32x4& va, u32x4& vb, const ChunkPair& cp
 }
 
 // Bound: memory (8 400 tokens of 32 + 2 x 8 heads of 128, 208 MB in 51 us, where a copy of as many bytes takes 42; the angles, the rotation in
-// 64 bits and non-temporal loads or stores do not show in it), latency for few tokens (one: 5.6 us).
+// 64 bits and non-temporal loads or stores do not show in it), latency for few tokens (one: 5.0 us).
 // One workgroup column per page that new tokens fall into; the column's waves share its jobs: K of a head, V of a head (the page's new tokens
 // in registers, with the cached ones where the page's scale or bounds need them), and runs of 256 pairs of chunks of Q.
 // The angles' cosines and sines are computed once per workgroup, in 64 bits, and kept as two 32-bit parts each: Q is rotated by the
@@ -403,17 +452,12 @@ __global__ __launch_bounds__(WG) void rope_append_kernel(const RopeParams p) {
 #pragma unroll
                     for (int k = 0; k < RUN; ++k) {
                         if ((base + 64 * k) / PPT >= s0 + n) continue;
-                        float f[8];
                         if constexpr (KVT == KV_BF16) {
-                            unpack8(x[k], f);
-                            lb.take(0, f);
-                            unpack8(y[k], f);
-                            lb.take(8, f);
+                            lb.take(0, x[k]);
+                            lb.take(4, y[k]);
                         } else {
-                            decode8(x[k].x, x[k].y, f);
-                            lb.take(0, f);
-                            decode8(x[k].z, x[k].w, f);
-                            lb.take(8, f);
+                            lb.take_codes(0, x[k].x, x[k].y);
+                            lb.take_codes(4, x[k].z, x[k].w);
                         }
                     }
                 }
@@ -446,45 +490,6 @@ __device__ __forceinline__ Row row_of(const Row* rows, int n, int idx, F&& start
 #pragma unroll
     for (int i = 0; i < W; ++i) out.w[i] = __builtin_amdgcn_readlane(r < 64 ? x.w[i] : y.w[i], r & 63);
     return __builtin_bit_cast(Row, out);
-}
-
-template <int CTRL>
-__device__ __forceinline__ uint32_t add_dpp(uint32_t x) {
-    return x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
-}
-// the sum over the 16 lanes of a row, in all of them
-__device__ __forceinline__ uint32_t row_sum(uint32_t x) {
-    x = add_dpp<0xB1>(x);                             // quad_perm [1, 0, 3, 2]
-    x = add_dpp<0x4E>(x);                             // quad_perm [2, 3, 0, 1]
-    x = add_dpp<0x124>(x);                            // row_ror:4
-    return add_dpp<0x128>(x);                         // row_ror:8
-}
-
-__device__ __forceinline__ uint32_t max16x2(uint32_t a, uint32_t b) {
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
-template <int CTRL>
-__device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
-    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
-    x = max_dpp<0xB1>(x);
-    x = max_dpp<0x4E>(x);
-    x = max_dpp<0x124>(x);
-    x = max_dpp<0x128>(x);
-    u32x2 r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = max(r[0], r[1]);
-    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return max(r[0], r[1]);
-}
-__device__ __forceinline__ uint32_t wave_umin(uint32_t x) { return ~wave_umax(~x); }
-__device__ __forceinline__ uint32_t wave_usum(uint32_t x) {
-    x = row_sum(x);
-    u32x2 r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = r[0] + r[1];
-    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return r[0] + r[1];
 }
 
 // bytes b < 128 -> -b: 128 - b has bit 7 set where b is 0 alone; with bit 7 flipped it is -b modulo 256
