@@ -805,7 +805,9 @@ __global__ __launch_bounds__(64 * SCORE_WAVES) void row_scores_kernel(const Sele
     }
 }
 
-// Scores of 16 groups x 16 pages at a time, SCORE_BATCH tiles in flight at once.
+// Scores of 16 groups x 16 pages at a time, SCORE_BATCH tiles in flight at once.  Bound: latency, and the trips of a tile's lines to the CUs.  (Codes,
+// scores and choice of 4 groups in one workgroup, the keys in LDS, instead of three launches: 35 us instead of 23 for 64 groups over 2 050 pages,
+// since every workgroup then takes all the pages' bounds.)
 template <int D>
 __global__ __launch_bounds__(64 * SCORE_WAVES) void page_scores_kernel(const SelectParams p, int heads) {
     constexpr int KK = D / 32, TB = SCORE_BATCH;
@@ -1462,8 +1464,10 @@ static void select_t(const SelectParams& p, int groups, int score_blocks, int64_
         }
     }
     const dim3 grid(groups, p.Hkv);
-    // (a wave alone with 16 keys a lane, and 4 waves with 16: 7.6 us instead of 6.7 for 768 choices of 128 to 1 024 pages, 7.5 instead of 6.0 for 4 of 2 176)
+    // As few waves as hold the keys in a few registers each: they meet at barriers.  (768 choices of 128 to 1 024 pages: a wave alone with 16 keys a lane
+    // 7.6 us, 4 waves with 4 6.7; 512 of 2 050: 8 waves with 8 8.4, 12 with 3 8.8, 4 with 9 7.1.)
     if (max_keys <= 4 * 64 * 4) hipLaunchKernelGGL((choose_pages_kernel<4, 4>), grid, dim3(256), 0, st, p);
+    else if (max_keys <= 4 * 64 * 10) hipLaunchKernelGGL((choose_pages_kernel<4, 10>), grid, dim3(256), 0, st, p);
     else if (max_keys <= 8 * 64 * 8) hipLaunchKernelGGL((choose_pages_kernel<8, 8>), grid, dim3(512), 0, st, p);
     else if (max_keys <= 16 * 64 * 16) hipLaunchKernelGGL((choose_pages_kernel<16, 16>), grid, dim3(1024), 0, st, p);
     else hipLaunchKernelGGL((choose_pages_kernel<16, 0>), grid, dim3(1024), 0, st, p);

@@ -224,7 +224,7 @@ def test_selection_of_groups(Hq, Hkv, d, P, g_tok):
         check_selection(codes, scale, table(g, C + L, P, 150), C, L, q, Hq, P, budget, first, last, g_tok)
 
 
-@pytest.mark.parametrize("pages", [1023, 1030, 4096, 4200, 16384, 16500, 40000])
+@pytest.mark.parametrize("pages", [1023, 1030, 2560, 2570, 4096, 4200, 16384, 16500, 40000])
 def test_selection_over_long_rows(pages):
     """Rows on either side of what each form of the choice holds in registers; scores with many equals among them."""
     case(f"select over {pages} pages")
