@@ -894,7 +894,7 @@ template <int NW, int KPL>
 __global__ __launch_bounds__(64 * NW) void choose_pages_kernel(const SelectParams p) {
     constexpr int BINS = 512, BPL = BINS / 64;
     __shared__ __attribute__((aligned(16))) uint32_t bins[BINS];
-    __shared__ uint32_t shared[2][NW];
+    __shared__ uint32_t range[2][NW], counts[2][NW];  // (two: with one value among all keys there is no barrier between them)
     const int lane = threadIdx.x & 63, wave = NW > 1 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : 0;
     const int item = blockIdx.x, h = blockIdx.y;
     const SelectRow r = row_of<SELECT_MAX_REQS>(p.rows, p.n, item, [](const SelectRow& x) { return x.item0; });
@@ -935,14 +935,14 @@ __global__ __launch_bounds__(64 * NW) void choose_pages_kernel(const SelectParam
     hi = wave_umax(hi);
     if constexpr (NW > 1) {
         if (lane == 0) {
-            shared[0][wave] = lo;
-            shared[1][wave] = hi;
+            range[0][wave] = lo;
+            range[1][wave] = hi;
         }
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            lo = min(lo, shared[0][w]);
-            hi = max(hi, shared[1][w]);
+            lo = min(lo, range[0][w]);
+            hi = max(hi, range[1][w]);
         }
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
@@ -1001,13 +1001,13 @@ __global__ __launch_bounds__(64 * NW) void choose_pages_kernel(const SelectParam
         above = wave_usum(above);
         equal = wave_usum(equal);
         if (lane == 0) {
-            shared[0][wave] = above;
-            shared[1][wave] = equal;
+            counts[0][wave] = above;
+            counts[1][wave] = equal;
         }
         __syncthreads();
         for (int w = 0; w < wave; ++w) {
-            const int take = min(left, (int)shared[1][w]);
-            at += (int)shared[0][w] + take;
+            const int take = min(left, (int)counts[1][w]);
+            at += (int)counts[0][w] + take;
             left -= take;
         }
     }

@@ -254,6 +254,22 @@ def test_selection_among_equal_scores_takes_the_lowest_pages():
         check_selection(codes, scale, bt, C, L, q, 4, P, budget, 1, 2, 1)
 
 
+@pytest.mark.parametrize("pages", [70, 1000, 2400, 4000, 9000, 17000])
+def test_selection_among_pages_of_one_score(pages):
+    """In every form of the choice: a row whose scores are one value, next to rows whose scores are two and many."""
+    case(f"select among {pages} pages of one score")
+    P, Hkv, d, n = 16, 4, 64, 64
+    g = np.random.default_rng(pages)
+    codes, scale = random_bounds(g, n, Hkv, d)
+    codes[:20], scale[:20] = 5, 1.0
+    codes[20], scale[20] = 9, 1.0
+    C, L = np.array([pages * P - 1, pages * P - 1, pages * P - 1], np.int32), np.ones(3, np.int32)
+    bt = np.stack([g.integers(0, 20, pages), g.integers(0, 21, pages), g.integers(0, n, pages)]).astype(np.int32)
+    q = normal_bits(g, 3, 8, d)
+    for budget in (9, 60):
+        check_selection(codes, scale, bt, C, L, q, 8, P, budget, 1, 2, 1)
+
+
 @pytest.mark.parametrize("mult", [1e-38, 1e-30, 1.0, 127.0, 1e30, 3e38])
 def test_selection_does_not_depend_on_the_size_of_the_queries(mult):
     case(f"select q x {mult}")
