@@ -1045,7 +1045,7 @@ struct ListLoader {
     int first[2];                                     // of the block that was fetched last: position of each half's first key (NONE: no page)
     int at[2];                                        // ... of the block that is committed
     float scale[4], sc[4];
-    static constexpr int NONE = 0x3fffffff;
+    static constexpr int NONE = 0x7fff0000;            // (positions end before 2^30; a block's keys, and differences of positions, stay in 32 bits)
 
     __device__ __forceinline__ void fetch_entries(const SparseParams& p, const int32_t* list, int key0, int step, int end, int j, int lane) {
         const int pos = key0 + (j + (lane >> 1) % IDS) * step + (lane & 1) * 16;

@@ -427,6 +427,32 @@ def test_pools_past_four_gigabytes():
     assert not big[0][:pages - p.n].any()
 
 
+def test_a_row_of_the_longest_length():
+    """2^30 tokens, nearly all on one page of the pool: the last page, alone or next to a page that is not there, is attended as in a short
+    row, and the selection finds the three pages that stand out and the lowest of the others."""
+    case("sparse longest row")
+    P, d = 16, 64
+    C, L = np.array([2 ** 30 - 1], np.int32), np.array([1], np.int32)
+    p = Pool(67, [2 * P], [0], 2, 1, d, P)
+    q = dev_bits(normal_bits(p.g, 1, 2, d))
+    last = 2 ** 30 // P - 1
+    bt = torch.full((1, last + 1), int(p.bt[0, 0]), dtype=torch.int32, device="cuda")
+    bt[0, last] = int(p.bt[0, 1])
+    for g_tok in (1, 20):
+        for there in ([last, -1], [-1, last], [last], [-1, -1, last, -1]):
+            sel = torch.tensor(there, dtype=torch.int32, device="cuda")[None, None]
+            got = A.sparse_attn(p.cache, C, L, bt, sel, q, group_tokens=g_tok)
+            short = torch.where(sel < 0, sel, torch.ones_like(sel))
+            assert torch.equal(got, A.sparse_attn(p.cache, [2 * P - 1], L, p.table, short, q, group_tokens=g_tok)), there
+    codes, scale = torch.ones((p.n, 1, 2, d), dtype=torch.int8, device="cuda"), torch.ones((p.n, 1), device="cuda")
+    other = int(np.setdiff1d(np.arange(p.n), p.bt[0])[0])
+    codes[other] = 3
+    high = [5, 2 ** 25 + 1, last - 1]
+    bt[0, high] = other
+    chosen = A.select_pages(p.cache, C, L, bt, A.PageBounds(codes, scale), q.abs(), 6)
+    assert chosen.flatten().tolist() == [0, 1, 5, 2 ** 25 + 1, last - 1, last]
+
+
 # ---- the operators together ----------------------------------------------------------------------------------------------------
 
 
