@@ -987,7 +987,7 @@ __global__ __launch_bounds__(64 * NW) void choose_pages_kernel(const SelectParam
         left -= (int)__builtin_amdgcn_readlane(above, owner);
         whole = (int)__builtin_amdgcn_readlane(inside, owner) == left;
         lo += bin << shift;
-        hi = min(hi, lo + ((1u << shift) - 1));
+        hi = lo + min(hi - lo, (1u << shift) - 1);    // (keys reach 2^32 - 1 where a page's scale is no number)
         if (NW > 1) __syncthreads();                  // before the bins are cleared again
     }
     if (whole) left = ch.n;

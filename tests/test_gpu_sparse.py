@@ -270,6 +270,27 @@ def test_selection_among_pages_of_one_score(pages):
         check_selection(codes, scale, bt, C, L, q, 8, P, budget, 1, 2, 1)
 
 
+@pytest.mark.parametrize("pages", [300, 2400, 20000])
+def test_selection_over_pages_whose_bounds_were_never_set(pages):
+    """Any bits in a page's scale: what is chosen among those pages is open, but it is a list of the row's pages, and nothing else is written."""
+    case(f"select over {pages} pages of any scale")
+    P, Hkv, d, n = 16, 2, 64, 500
+    g = np.random.default_rng(pages)
+    C, L, budget = np.array([pages * P - 1, 40 * P], np.int32), np.ones(2, np.int32), 24
+    bt = torch.from_numpy(table(g, C + L, P, n)).cuda()
+    q = dev_bits(normal_bits(g, 2, 2, d))
+    cache = A.KVCache(2, Hkv, d, P, None, None, 1.0)
+    for low, high in ((0, 2 ** 32), (0x7fffff00, 0x80000000), (0x7f800000, 0x80000000), (0xffffff00, 2 ** 32)):
+        codes = torch.from_numpy(random_bounds(g, n, Hkv, d)[0]).cuda()
+        scale = g.integers(low, high, (n, Hkv), dtype=np.uint32).view(np.float32)
+        out = torch.full((4, Hkv, budget), -7, dtype=torch.int32, device="cuda")
+        A.select_pages(cache, C, L, bt, A.PageBounds(codes, torch.from_numpy(scale).cuda()), q, budget, out=out[1:3])
+        out = out.cpu().numpy()
+        assert (out[[0, 3]] == -7).all()
+        for r in (0, 1):
+            assert (np.diff(out[1 + r], axis=1) > 0).all() and (out[1 + r, :, 0] == 0).all() and (out[1 + r, :, -1] == C[r] // P).all()
+
+
 @pytest.mark.parametrize("mult", [1e-38, 1e-30, 1.0, 127.0, 1e30, 3e38])
 def test_selection_does_not_depend_on_the_size_of_the_queries(mult):
     case(f"select q x {mult}")
