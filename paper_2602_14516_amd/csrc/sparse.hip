@@ -895,7 +895,7 @@ __global__ __launch_bounds__(64 * NW) void choose_pages_kernel(const SelectParam
     constexpr int BINS = 512, BPL = BINS / 64;
     __shared__ __attribute__((aligned(16))) uint32_t bins[BINS];
     __shared__ uint32_t range[2][NW], counts[2][NW];  // (two: with one value among all keys there is no barrier between them)
-    const int lane = threadIdx.x & 63, wave = NW > 1 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : 0;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int item = blockIdx.x, h = blockIdx.y;
     const SelectRow r = row_of<SELECT_MAX_REQS>(p.rows, p.n, item, [](const SelectRow& x) { return x.item0; });
     const int grp = item - r.item0;
@@ -933,17 +933,15 @@ __global__ __launch_bounds__(64 * NW) void choose_pages_kernel(const SelectParam
     });
     lo = wave_umin(lo);
     hi = wave_umax(hi);
-    if constexpr (NW > 1) {
-        if (lane == 0) {
-            range[0][wave] = lo;
-            range[1][wave] = hi;
-        }
-        __syncthreads();
+    if (lane == 0) {
+        range[0][wave] = lo;
+        range[1][wave] = hi;
+    }
+    __syncthreads();
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            lo = min(lo, range[0][w]);
-            hi = max(hi, range[1][w]);
-        }
+    for (int w = 0; w < NW; ++w) {
+        lo = min(lo, range[0][w]);
+        hi = max(hi, range[1][w]);
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
@@ -988,28 +986,27 @@ __global__ __launch_bounds__(64 * NW) void choose_pages_kernel(const SelectParam
         whole = (int)__builtin_amdgcn_readlane(inside, owner) == left;
         lo += bin << shift;
         hi = lo + min(hi - lo, (1u << shift) - 1);    // (keys reach 2^32 - 1 where a page's scale is no number)
-        if (NW > 1) __syncthreads();                  // before the bins are cleared again
+        __syncthreads();                              // before the bins are cleared again
     }
     if (whole) left = ch.n;
     int at = ch.nfirst;
-    if constexpr (NW > 1) {                           // what the waves before this one take
-        uint32_t above = 0, equal = 0;
-        each([&](uint32_t k, int, bool there) {
-            above += there && k > hi ? 1u : 0u;
-            equal += there && k >= lo && k <= hi ? 1u : 0u;
-        });
-        above = wave_usum(above);
-        equal = wave_usum(equal);
-        if (lane == 0) {
-            counts[0][wave] = above;
-            counts[1][wave] = equal;
-        }
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) {
-            const int take = min(left, (int)counts[1][w]);
-            at += (int)counts[0][w] + take;
-            left -= take;
-        }
+    // what the waves before this one take
+    uint32_t above = 0, equal = 0;
+    each([&](uint32_t k, int, bool there) {
+        above += there && k > hi ? 1u : 0u;
+        equal += there && k >= lo && k <= hi ? 1u : 0u;
+    });
+    above = wave_usum(above);
+    equal = wave_usum(equal);
+    if (lane == 0) {
+        counts[0][wave] = above;
+        counts[1][wave] = equal;
+    }
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) {
+        const int take = min(left, (int)counts[1][w]);
+        at += (int)counts[0][w] + take;
+        left -= take;
     }
     each([&](uint32_t k, int i, bool there) {
         const bool equal = there && k >= lo && k <= hi;
@@ -1156,8 +1153,9 @@ constexpr int sparse_smem() {
 // Logits, running maximum, sum and output are held in 32 bits; the probabilities are rounded to bf16 for the second product alone, which the
 // matrix cores take in 16 bits (their sum is taken before).
 // Bound: memory where every list is another's (96 rows x 8 heads over 128 pages of 16, 809 MB in 130 us = 6.2 TB/s); LDS, through which K and V
-// pass on their way into the operands' layout, where 32 rows share a list that is in L2 (64 groups: 40 us, on pages that never leave L2 38; K loaded
-// straight in the layout of a 32x32x16 or two 16x16x32 products, quarter or half lines at a time, 52 and 50).
+// pass on their way into the operands' layout, where 32 rows share a list that is in L2 (64 groups: 40 us, on pages that never leave L2 38, without its
+// products 31, without its loads 33, without what it writes to LDS 35: the three overlap but for a fifth, with two waves a SIMD; K loaded straight in
+// the layout of a 32x32x16 or two 16x16x32 products, quarter or half lines at a time, 52 and 50).
 template <int D, int KVT, int ROWS, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparseParams p) {
     using G_ = Geo<D>;
