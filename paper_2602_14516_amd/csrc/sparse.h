@@ -32,7 +32,7 @@ constexpr int SCORE_WAVES = 4;
 inline int score_heads(int Hkv) { return Hkv > 2 ? 4 : Hkv; }
 inline int score_pages(int Hkv, int score_tiles) { return score_tiles * 16 * (SCORE_WAVES / score_heads(Hkv)); }
 inline int score_tiles(int64_t tiles) {
-    const int64_t t = tiles / 3072 / SCORE_BATCH * SCORE_BATCH;
+    const int64_t t = tiles / 3000 / SCORE_BATCH * SCORE_BATCH;
     return (int)(t < SCORE_BATCH ? SCORE_BATCH : t > 64 ? 64 : t);
 }
 
