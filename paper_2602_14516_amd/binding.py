@@ -537,6 +537,11 @@ def _want_bounds(cache: KVCache, bounds: PageBounds):
     _want("bounds.scale", bounds.scale, "float32", (n, cache.num_kv_heads))
 
 
+def _want_workspace(workspace):
+    if not workspace.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor is wanted (strides {tuple(workspace.stride())} for {tuple(workspace.shape)})")
+
+
 def _rows(name, t, tokens, heads, d):
     """[tokens, heads, d] with the heads of a token next to each other: elements from token to token."""
     import torch
@@ -553,6 +558,15 @@ def _lengths(ctx_len, incr_len):
     if ctx.shape != inc.shape or ctx.ndim != 1:
         raise ValueError(f"ctx_len and incr_len: two vectors of one length are wanted, not {ctx.shape} and {inc.shape}")
     return ctx, inc
+
+
+def _output(name, shape, dtype, q, stream):
+    """A result of a call on `stream`, from that stream's memory."""
+    import torch
+    if isinstance(stream, int) and stream != torch.cuda.current_stream().cuda_stream:
+        raise ValueError(f"pass {name}= when stream= is a raw stream handle other than torch's current stream")
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
+        return torch.empty(shape, dtype=getattr(torch, dtype), device=q.device)
 
 
 def num_groups(incr_len, group_tokens=1) -> int:
@@ -573,7 +587,6 @@ def rope_kv_append(cache: KVCache, ctx_len, incr_len, block_table, rope: Rope, q
         if st is not None:
             _check(st, "ampd_rope_kv_append")
             return q_out
-    import torch
     ctx, inc = _lengths(ctx_len, incr_len)
     n = int(inc.sum())
     _want_table(block_table, len(ctx))
@@ -589,8 +602,7 @@ def rope_kv_append(cache: KVCache, ctx_len, incr_len, block_table, rope: Rope, q
     if bounds is not None:
         _want_bounds(cache, bounds)
     if q is not None and q_out is None:
-        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
-            q_out = torch.empty((n, cache.num_q_heads, d), dtype=torch.bfloat16, device=q.device)
+        q_out = _output("q_out", (n, cache.num_q_heads, d), "bfloat16", q, stream)
     if q is not None:
         _want("q_out", q_out, "bfloat16", (n, cache.num_q_heads, d))
     _same_device((("k_pool", cache.k_pool), ("v_pool", cache.v_pool), ("k_scale", cache.k_scale), ("v_scale", cache.v_scale),
@@ -643,21 +655,20 @@ def select_pages(cache: KVCache, ctx_len, incr_len, block_table, bounds: PageBou
         if st is not None:
             _check(st, "ampd_select_pages")
             return out
-    import torch
     ctx, inc = _lengths(ctx_len, incr_len)
     _want_table(block_table, len(ctx))
     _want_bounds(cache, bounds)
     _want("q", q, "bfloat16", (int(inc.sum()), cache.num_q_heads, cache.head_dim))
     shape = (num_groups(inc, group_tokens), cache.num_kv_heads, int(budget))
     if out is None:
-        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
-            out = torch.empty(shape, dtype=torch.int32, device=q.device)
+        out = _output("out", shape, "int32", q, stream)
     _want("out", out, "int32", shape)
     s = _selection(budget, first_pages, last_pages, group_tokens)
     b, keep = _batch_arg(ctx, inc, block_table, block_table_host)
     c = _selecting_cache(cache, bounds)
     if workspace is None:
         workspace = _temp_workspace(int(_packed.ampd_select_pages_workspace_bytes(c, b, ctypes.byref(s))), q, stream)
+    _want_workspace(workspace)
     _same_device((("block_table", block_table), ("bounds", bounds.codes), ("bounds", bounds.scale), ("q", q), ("out", out), ("workspace", workspace)))
     _check(_packed.ampd_select_pages(c, b, ctypes.byref(_Bounds(_ptr(bounds.codes), _ptr(bounds.scale))), ctypes.byref(s), _ptr(q), _ptr(out), _ptr(workspace),
                                      workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ampd_select_pages")
@@ -688,7 +699,6 @@ def sparse_attn(cache: KVCache, ctx_len, incr_len, block_table, selected, q, *, 
         if st is not None:
             _check(st, "ampd_sparse_attn")
             return out
-    import torch
     ctx, inc = _lengths(ctx_len, incr_len)
     _want_table(block_table, len(ctx))
     _want_pools(cache)
@@ -699,13 +709,13 @@ def sparse_attn(cache: KVCache, ctx_len, incr_len, block_table, selected, q, *, 
         raise ValueError(f"selected: [{num_groups(inc, group_tokens)}, {cache.num_kv_heads}, budget] is wanted, not {tuple(selected.shape)}")
     budget = int(selected.shape[2])
     if out is None:
-        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
-            out = torch.empty_like(q)
+        out = _output("out", shape, "bfloat16", q, stream)
     _want("out", out, "bfloat16", shape)
     b, keep = _batch_arg(ctx, inc, block_table, block_table_host)
     c = _cache_arg(cache)
     if workspace is None:
         workspace = _temp_workspace(int(_packed.ampd_sparse_attn_workspace_bytes(c, b, budget, int(group_tokens))), q, stream)
+    _want_workspace(workspace)
     _same_device((("k_pool", cache.k_pool), ("v_pool", cache.v_pool), ("k_scale", cache.k_scale), ("v_scale", cache.v_scale), ("block_table", block_table),
                   ("selected", selected), ("q", q), ("out", out), ("workspace", workspace)))
     _check(_packed.ampd_sparse_attn(c, b, _ptr(selected), budget, int(group_tokens), _ptr(q), _ptr(out), _ptr(workspace),

@@ -362,7 +362,7 @@ PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
                 return false;
             const at::Tensor* w;
             if (!x.bounds(a[5], &bounds) || !x.want(a[6], at::kBFloat16, {x.tokens, x.c.num_q_heads, x.c.head_dim}, &q) ||
-                !x.want(a[11], at::kInt, {x.groups(s.group_tokens), x.c.num_kv_heads, s.budget}, &out) || !tensor(a[12], &w) || !x.there(*w))
+                !x.want(a[11], at::kInt, {x.groups(s.group_tokens), x.c.num_kv_heads, s.budget}, &out) || !tensor(a[12], &w) || !x.there(*w) || !w->is_contiguous())
                 return false;
             ws = w->data_ptr();
             bytes = w->nbytes();
@@ -387,7 +387,7 @@ PyObject* sparse_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
             budget = (int32_t)t->size(2);
             if (!x.want(a[5], at::kInt, {x.groups(group), x.c.num_kv_heads, budget}, &sel) ||
                 !x.want(a[6], at::kBFloat16, {x.tokens, x.c.num_q_heads, x.c.head_dim}, &q) ||
-                !x.want(a[8], at::kBFloat16, {x.tokens, x.c.num_q_heads, x.c.head_dim}, &out) || !tensor(a[9], &w) || !x.there(*w))
+                !x.want(a[8], at::kBFloat16, {x.tokens, x.c.num_q_heads, x.c.head_dim}, &out) || !tensor(a[9], &w) || !x.there(*w) || !w->is_contiguous())
                 return false;
             ws = w->data_ptr();
             bytes = w->nbytes();

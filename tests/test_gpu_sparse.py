@@ -655,3 +655,26 @@ def test_what_the_library_would_read_as_something_else_is_refused_on_the_device_
         with pytest.raises(A.AmpdError) as e:
             f()
         assert e.value.status == status
+
+
+def test_results_and_workspaces_a_raw_stream_or_a_view_cannot_have():
+    """A raw handle of another stream names no memory to allocate results from; a workspace's bytes lie next to each other."""
+    case("sparse raw streams and workspace views")
+    p, out, calls = session()
+    for f in calls:
+        f()
+    C, L = np.array([60, 33], np.int32), np.array([1, 9], np.int32)
+    q, sel, raw = out["q_out"], out["sel"], torch.cuda.Stream().cuda_stream
+    rope, kv = A.Rope(torch.ones(32, device="cuda")), q[:, :2]
+    with pytest.raises(ValueError, match="pass q_out="):
+        A.rope_kv_append(p.cache, C, L, p.table, rope, q, kv, kv, stream=raw)
+    with pytest.raises(ValueError, match="pass out="):
+        A.select_pages(p.cache, C, L, p.table, p.bounds, q, 4, group_tokens=4, workspace=out["ws"], stream=raw)
+    with pytest.raises(ValueError, match="pass workspace="):
+        A.sparse_attn(p.cache, C, L, p.table, sel, q, group_tokens=4, out=out["out"], stream=raw)
+    view = torch.empty(1, dtype=torch.uint8, device="cuda").expand(1 << 20)
+    for stream in (None, torch.cuda.current_stream()):
+        with pytest.raises(ValueError, match="workspace"):
+            A.select_pages(p.cache, C, L, p.table, p.bounds, q, 4, group_tokens=4, out=sel, workspace=view, stream=stream)
+        with pytest.raises(ValueError, match="workspace"):
+            A.sparse_attn(p.cache, C, L, p.table, sel, q, group_tokens=4, out=out["out"], workspace=view, stream=stream)
