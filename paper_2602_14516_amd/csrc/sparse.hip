@@ -413,7 +413,7 @@ __global__ __launch_bounds__(WG) void rope_append_kernel(const RopeParams p) {
                 const bool raise = s0 > 0 && e > e_old;
                 if (s0 > 0 && !raise) e = e_old;
                 const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-                const float f = __uint_as_float((uint32_t)(e_old - e + 127) << 23);     // (used where the exponent rises: 2^(e_old - e))
+                const float f = reencode_factor(e_old, e);                               // (used where the exponent rises)
 #pragma unroll
                 for (int k = 0; k < RUN; ++k) {
                     const int s = (base + 64 * k) / PPT;

@@ -453,9 +453,12 @@ __device__ __forceinline__ float page_amax(const char* src, int64_t row_bytes, i
     for (int u = t; u < n * cph; u += nthr) amax = fmaxf(amax, chunk_amax(new_chunk(src, row_bytes, u, cph)));
     return amax;
 }
+// 2^(e_old - e) for the codes of a page whose exponent rises to e; the exponents are up to 159 apart, and below 2^-126 every code becomes a
+// zero of its sign (448 * 2^-127 is far below half the smallest code).
+__device__ __forceinline__ float reencode_factor(int e_old, int e) { return __uint_as_float((uint32_t)max(0, e_old - e + 127) << 23); }
 // the page's first n_old slots held codes of exponent e_old: re-encode them for e > e_old
 __device__ __forceinline__ void page_reencode(uint8_t* pg, int n_old, int D, int e_old, int e, int t, int nthr) {
-    const float f = __uint_as_float((uint32_t)(e_old - e + 127) << 23);     // 2^(e_old - e)
+    const float f = reencode_factor(e_old, e);
     for (int u = t; u < n_old * (D / 4); u += nthr) {
         uint32_t* q4 = reinterpret_cast<uint32_t*>(pg) + u;
         const uint32_t w = *q4;
