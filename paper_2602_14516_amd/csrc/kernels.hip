@@ -609,14 +609,7 @@ struct NewToken {
         if (carries(lane)) s_old = *scale(p, ic, page, lane);
     }
     __device__ __forceinline__ void finish(const AttnParams& p, const ItemCtx& ic, int lane) {
-        const uint32_t w[4] = {row.x, row.y, row.z, row.w};
-        float f[8], amax = 0.0f;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            f[2 * x] = __uint_as_float(w[x] << 16);
-            f[2 * x + 1] = __uint_as_float(w[x] & 0xffff0000u);
-            amax = fmaxf(amax, fmaxf(fabsf(f[2 * x]), fabsf(f[2 * x + 1])));
-        }
+        float amax = chunk_amax(row);
 #pragma unroll
         for (int o = CPK / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
         const int slot = ic.C & (p.P - 1);                    // = tokens the page already holds
@@ -634,7 +627,7 @@ struct NewToken {
         e = max(e, e_old);
         if (carries(lane)) {
             const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-            const u32x2 o = {encode4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), encode4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)};
+            const u32x2 o = encode_chunk(row, inv);
             uint8_t* pg = static_cast<uint8_t*>(const_cast<void*>(is_v(lane) ? p.v_pool : p.k_pool)) + tile;
             *reinterpret_cast<u32x2*>(pg + slot * D + (lane % CPK) * 8) = o;
             if (lane % CPK == 0) *scale(p, ic, page, lane) = __uint_as_float((uint32_t)(e + 127) << 23);

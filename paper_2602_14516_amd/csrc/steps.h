@@ -445,6 +445,10 @@ __device__ __forceinline__ u32x2 encode_chunk(const u32x4& v, float inv) {
         f[2 * x] = __uint_as_float(w[x] << 16) * inv;
         f[2 * x + 1] = __uint_as_float(w[x] & 0xffff0000u) * inv;
     }
+    if (inv <= 0x1p-119f) {                           // the exponent is clamped: finite numbers saturate (the conversion makes them NaN from 464 on)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) f[x] = fabsf(f[x]) > 448.0f && fabsf(f[x]) < 512.0f ? copysignf(448.0f, f[x]) : f[x];
+    }
     return u32x2{encode4(f[0], f[1], f[2], f[3]), encode4(f[4], f[5], f[6], f[7])};
 }
 // this thread's largest magnitude
@@ -467,7 +471,7 @@ __device__ __forceinline__ void page_reencode(uint8_t* pg, int n_old, int D, int
         *q4 = encode4(lo.x * f, lo.y * f, hi.x * f, hi.y * f);
     }
 }
-// encode the new tokens into the slots from dst on: x * 2^-e, |.| <= 448 by construction
+// encode the new tokens into the slots from dst on: x * 2^-e
 __device__ __forceinline__ void page_encode(uint8_t* dst, const char* src, int64_t row_bytes, int n, int D, int e, int t, int nthr) {
     const int cph = D / 8;
     const float inv = __uint_as_float((uint32_t)(127 - e) << 23);

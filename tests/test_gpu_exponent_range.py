@@ -52,3 +52,25 @@ def test_old_codes_follow_an_exponent_that_rises_by_any_amount(way, Hkv, d, P, L
     if way == "rotate_with_bounds":
         p.set_bounds(C, inc)
         p.assert_bounds_equal()
+
+
+@pytest.mark.parametrize("way", ["append", "attention", "rotate"])
+def test_numbers_above_the_largest_scale_saturate(way):
+    """Finite bf16 numbers from 448 * 2^119 up to the largest, in a fresh page and in one that holds tokens."""
+    print(f"case: {way}, largest numbers", flush=True)
+    Hkv, d, P = 2, 64, 16
+    C, inc = np.array([0, 3, 16, 30], np.int32), np.array([2, 1, 3, 4], np.int32)
+    p = Pool(9, C, inc, 4, Hkv, d, P, True)
+    m = int(inc.sum())
+    bits = np.uint16(0x7F60) + p.g.integers(0, 0x20, (2, m, Hkv, d)).astype(np.uint16)
+    bits |= (p.g.integers(0, 2, bits.shape) << 15).astype(np.uint16)
+    k, v = bits
+    if way == "append":
+        A.kv_append(p.cache, C, inc, p.table, dev_bits(k), dev_bits(v))
+    elif way == "attention":
+        A.mixed_batch_attn(p.cache, C, inc, p.table, dev_bits(normal_bits(p.g, m, 4, d)), dev_bits(k), dev_bits(v))
+    else:
+        A.rope_kv_append(p.cache, C, inc, p.table, A.Rope(torch.zeros(d // 2, device="cuda")), None, dev_bits(k), dev_bits(v))
+    torch.cuda.synchronize()
+    p.append(C, inc, k, v)
+    p.assert_pools_equal()
