@@ -495,9 +495,10 @@ __device__ __forceinline__ Row row_of(const Row* rows, int n, int idx, F&& start
 // bytes b < 128 -> -b: 128 - b has bit 7 set where b is 0 alone; with bit 7 flipped it is -b modulo 256
 __device__ __forceinline__ uint32_t negate_bytes(uint32_t x) { return (0x80808080u - x) ^ 0x80808080u; }
 
-// 2^-f for the smallest f with amax <= 127 * 2^f, in two factors: f reaches -133 and 123 (a group of zeros: any)
+// 2^-f for the smallest f with amax <= 127 * 2^f, in two factors: f reaches -139 (one step above zero) and 122 (a group of zeros: any)
 __device__ __forceinline__ void query_step(uint32_t amax_bits, float& m0, float& m1) {
-    const int ex = (int)(amax_bits >> 23) - 127, f = (amax_bits & 0x7fffffu) <= 0x7e0000u ? ex - 6 : ex - 5;
+    const float amax = __uint_as_float(amax_bits);    // = mantissa in [0.5, 1) * 2^x, numbers without a leading one included
+    const int x = __builtin_amdgcn_frexp_expf(amax), f = __builtin_amdgcn_frexp_mantf(amax) <= 0.9921875f ? x - 7 : x - 6;
     const int fs = max(-126, min(127, -f));
     m0 = __uint_as_float((uint32_t)(fs + 127) << 23);
     m1 = __uint_as_float((uint32_t)(max(-126, min(127, -f - fs)) + 127) << 23);
