@@ -236,7 +236,8 @@ ampd_status ampd_paged_attn(const ampd_kv_cache *cache, const ampd_batch *batch,
  * ampd_kv_unpack, an attention call that appends).
  * All of them take their lengths as kernel arguments, enqueue kernels only and touch no staging buffer, so they may be
  * recorded into a graph; a replay repeats the call with the lengths it was recorded with.  Physical page ids of the block
- * table outside [0, num_pages) are skipped: such a page is neither written nor attended. */
+ * table outside [0, num_pages) are skipped: such a page is neither written nor attended, and among the pages that a selection
+ * takes by their score it comes behind all others. */
 
 /* Position rotation: element pair (x1, x2) of a head at position t becomes
  * scale * (x1 cos a - x2 sin a, x2 cos a + x1 sin a), a = t * inv_freq[j] (the product and its cosine and sine in 64 bits).

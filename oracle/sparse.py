@@ -103,8 +103,10 @@ def select_reference(codes, scale, block_table, ctx_len, incr_len, q, P, budget,
             pick = list(always)
             if left > 0:
                 pages = np.asarray(block_table[r])[rest]
+                there = (pages >= 0) & (pages < len(codes))                     # the others come last
+                pages = np.where(there, pages, 0)
                 s = page_scores(q[row:row + m, h * G:(h + 1) * G].reshape(m * G, -1), codes[pages, h], scale[pages, h])
-                pick += [rest[j] for j in np.argsort(-s.astype(np.float64), kind="stable")[:left]]
+                pick += [rest[j] for j in np.argsort(-np.where(there, s.astype(np.float64), -np.inf), kind="stable")[:left]]
             out[i, h, :len(pick)] = sorted(pick)
     return out
 

@@ -685,10 +685,10 @@ __global__ __launch_bounds__(64) void query_codes_kernel(const SelectParams p) {
     }
 }
 
-// Scores as 32-bit numbers that order as the scores do.
-__device__ __forceinline__ uint32_t ordered(float x) {
+// Scores as 32-bit numbers that order as the scores do; a page without a place in the pool (there: false) comes behind every score.
+__device__ __forceinline__ uint32_t ordered(float x, bool there) {
     const uint32_t u = __float_as_uint(x);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    return there ? u & 0x80000000u ? ~u : u | 0x80000000u : 0u;
 }
 
 // A tile of 16 pages: their bounds of one KV head, as the second operand of the 16x16x64 whole-number product (lane l: bytes 16 (l / 16) .. of
@@ -697,8 +697,10 @@ template <int D>
 struct PageTile {
     i32x4 b[D / 32];
     float scale;
+    bool there;
     __device__ __forceinline__ void load(const SelectParams& p, int id, int h, int lane) {
-        const int64_t ph = (int64_t)((uint32_t)id < (uint64_t)p.num_pages ? id : 0) * p.Hkv + h;
+        there = (uint32_t)id < (uint64_t)p.num_pages;
+        const int64_t ph = (int64_t)(there ? id : 0) * p.Hkv + h;
         const int8_t* src = p.codes + ph * (2 * D) + (lane >> 4) * 16;
 #pragma unroll
         for (int kk = 0; kk < D / 32; ++kk) b[kk] = *reinterpret_cast<const i32x4*>(src + kk * 64);
@@ -713,7 +715,7 @@ struct PageTile {
             hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(limb[1][kk], b[kk], hi, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) key[i] = ordered((float)(hi[i] * 128 + lo[i]) * scale);
+        for (int i = 0; i < 4; ++i) key[i] = ordered((float)(hi[i] * 128 + lo[i]) * scale, there);
     }
 };
 
@@ -753,7 +755,7 @@ __global__ __launch_bounds__(64 * SCORE_WAVES) void row_scores_kernel(const Sele
     const int mine = min(lane % LPP, NL - 1) * PPI + lane / LPP;
     auto page_id = [&](int first) {
         const int id = bt[min(first + mine, end - 1)];
-        return (uint32_t)id < (uint64_t)p.num_pages ? id : 0;
+        return (uint32_t)id < (uint64_t)p.num_pages ? id : -1;
     };
     int id[TB];
 #pragma unroll
@@ -766,14 +768,16 @@ __global__ __launch_bounds__(64 * SCORE_WAVES) void row_scores_kernel(const Sele
     for (int at = w.pg0; at < end; at += TB * 16) {
         i32x4 b[TB][NL];
         float scale[TB];
+        bool there[TB];
 #pragma unroll
         for (int t = 0; t < TB; ++t) {
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
-                const int page = __shfl(id[t], (lane & ~(LPP - 1)) + i, 64);
+                const int page = max(0, __shfl(id[t], (lane & ~(LPP - 1)) + i, 64));
                 b[t][i] = *reinterpret_cast<const i32x4*>(p.codes + ((int64_t)page * p.Hkv + h) * (2 * D) + (lane % LPP) * 16);
             }
-            scale[t] = p.bscale[(int64_t)id[t] * p.Hkv + h];
+            scale[t] = p.bscale[(int64_t)max(0, id[t]) * p.Hkv + h];
+            there[t] = id[t] >= 0;
         }
 #pragma unroll
         for (int t = 0; t < TB; ++t) id[t] = page_id(at + (TB + t) * 16);
@@ -801,7 +805,7 @@ __global__ __launch_bounds__(64 * SCORE_WAVES) void row_scores_kernel(const Sele
                 n = i == lane % LPP ? (int)s : n;
             }
             const int page = at + t * 16 + mine;
-            if (lane % LPP < NL && page < end) keys[page] = ordered((float)n * scale[t]);
+            if (lane % LPP < NL && page < end) keys[page] = ordered((float)n * scale[t], there[t]);
         }
     }
 }
