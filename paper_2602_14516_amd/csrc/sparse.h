@@ -16,9 +16,9 @@ inline int64_t groups_of(int64_t L, int g) { return (L + g - 1) / g; }
 
 // Scores of a row's pages, for one group and KV head: this many 32-bit keys.
 inline int64_t key_stride(int64_t T, int P) { return ((T + P - 1) / P + 63) / 64 * 64; }
-// A launch scores at most this many keys, or those of a single group: the workspace stays at 64 MiB where rows are many or long, and what
-// one launch writes the next one finds in the last-level cache.
-constexpr int64_t SELECT_KEYS = 16 << 20;
+// A launch writes at most this many 32-bit words, keys and query codes together, or those of a single group: the workspace stays at 64 MiB
+// where rows are many or long, and what one launch writes the next one finds in the last-level cache.
+constexpr int64_t SELECT_WORDS = 16 << 20;
 
 // Row tile of a sparse-attention workgroup: 16 query rows, or 32 where a group has more.
 inline int sparse_tile(int rows) { return rows <= 16 ? 16 : 32; }
@@ -50,7 +50,9 @@ struct SelectRow {
 };
 struct SelectLaunch {
     int n = 0, groups = 0, score_blocks = 0, score_tiles = 0;
-    int64_t keys = 0;         // in the workspace
+    bool codes = false;       // the queries' codes are made by a launch of their own (some row has more than one group, and scores are wanted)
+    int64_t keys = 0;         // in the workspace; the codes follow
+    int64_t code_offset() const { return (keys + 63) / 64 * 256; }       // bytes
     int64_t max_keys = 0;     // the most pages that a group chooses from
     SelectRow rows[SELECT_MAX_REQS];
 };
@@ -97,7 +99,6 @@ ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const a
 ampd_status sparse_launches(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, int32_t group_tokens, LaunchFn<SparseLaunch> f);
 // What a call needs of its workspace, and its launch where it has one alone (the usual case: it is then not worked out twice).
 struct SelectPlan {
-    int64_t keys_bytes = 0;   // of the keys; the query codes follow
     int64_t bytes = 0;
     int launches = 0;
     SelectLaunch only;
@@ -177,7 +178,7 @@ struct SparseParams {
 
 hipError_t launch_rope(RopeParams& p, int kvt, int64_t pages, int max_new, hipStream_t st);
 hipError_t launch_bounds(BoundsParams& p, int kvt, int64_t pages, hipStream_t st);
-hipError_t launch_select(const SelectParams& p, int D, int groups, int score_blocks, int64_t max_keys, hipStream_t st);
+hipError_t launch_select(const SelectParams& p, int D, int groups, int score_blocks, bool codes, int64_t max_keys, hipStream_t st);
 hipError_t launch_sparse(const SparseParams& p, int D, int kvt, int groups, int waves, hipStream_t st);
 
 }  // namespace ampd

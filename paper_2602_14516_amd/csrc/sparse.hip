@@ -1453,13 +1453,11 @@ hipError_t launch_bounds(BoundsParams& p, int kvt, int64_t pages, hipStream_t st
 }
 
 template <int D>
-static void select_t(const SelectParams& p, int groups, int score_blocks, int64_t max_keys, hipStream_t st) {
-    bool one = true;
-    for (int i = 0; i < p.n; ++i) one &= p.rows[i].L <= p.g;
+static void select_t(const SelectParams& p, int groups, int score_blocks, bool codes, int64_t max_keys, hipStream_t st) {
     if (score_blocks > 0) {
         const int heads = score_heads(p.Hkv);
         const dim3 grid(score_blocks, (p.Hkv + heads - 1) / heads);
-        if (one) {
+        if (!codes) {
             hipLaunchKernelGGL((row_scores_kernel<D>), grid, dim3(64 * SCORE_WAVES), 0, st, p, heads);
         } else {
             hipLaunchKernelGGL((query_codes_kernel<D>), dim3(groups, p.Hkv), dim3(64), 0, st, p);
@@ -1476,11 +1474,11 @@ static void select_t(const SelectParams& p, int groups, int score_blocks, int64_
     else hipLaunchKernelGGL((choose_pages_kernel<16, 0>), grid, dim3(1024), 0, st, p);
 }
 
-// groups: of this launch; score_blocks: workgroup columns of the score launch (0: every group takes all its pages); max_keys: the most pages
-// a group chooses from
-hipError_t launch_select(const SelectParams& p, int D, int groups, int score_blocks, int64_t max_keys, hipStream_t st) {
-    if (D == 128) select_t<128>(p, groups, score_blocks, max_keys, st);
-    else select_t<64>(p, groups, score_blocks, max_keys, st);
+// groups: of this launch; score_blocks: workgroup columns of the score launch (0: every group takes all its pages); codes: some row has more
+// than one group; max_keys: the most pages a group chooses from
+hipError_t launch_select(const SelectParams& p, int D, int groups, int score_blocks, bool codes, int64_t max_keys, hipStream_t st) {
+    if (D == 128) select_t<128>(p, groups, score_blocks, codes, max_keys, st);
+    else select_t<64>(p, groups, score_blocks, codes, max_keys, st);
     return hipGetLastError();
 }
 

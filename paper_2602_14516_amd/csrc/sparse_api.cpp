@@ -121,7 +121,6 @@ ampd_status ampd_select_pages(const ampd_kv_cache* cache, const ampd_batch* batc
     p.block_table = batch->d_block_table;
     p.selected = selected;
     p.keys = static_cast<uint32_t*>(workspace);
-    p.qcodes = static_cast<int8_t*>(workspace) + plan.keys_bytes;
     p.num_pages = cache->num_pages;
     p.Hq = cache->num_q_heads;
     p.Hkv = cache->num_kv_heads;
@@ -133,10 +132,11 @@ ampd_status ampd_select_pages(const ampd_kv_cache* cache, const ampd_batch* batc
     p.last = sel->last_pages;
     p.g = sel->group_tokens;
     auto launch = [&](const SelectLaunch& l) {
+        p.qcodes = static_cast<int8_t*>(workspace) + l.code_offset();
         p.score_tiles = l.score_tiles;
         p.n = l.n;
         std::memcpy(p.rows, l.rows, l.n * sizeof(SelectRow));
-        return launch_select(p, cache->head_dim, l.groups, l.score_blocks, l.max_keys, static_cast<hipStream_t>(stream)) == hipSuccess ? AMPD_OK : AMPD_ERR_HIP;
+        return launch_select(p, cache->head_dim, l.groups, l.score_blocks, l.codes, l.max_keys, static_cast<hipStream_t>(stream)) == hipSuccess ? AMPD_OK : AMPD_ERR_HIP;
     };
     return plan.launches == 1 ? launch(plan.only) : select_launches(cache, batch, sel, launch);
 }

@@ -69,7 +69,9 @@ ampd_status validate_sparse(const ampd_kv_cache* c, const ampd_batch* b, int32_t
 ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* s, LaunchFn<SelectLaunch> f) {
     const int P = c->page_size, logP = log2_exact(P), g = s->group_tokens, Hkv = c->num_kv_heads;
     const int64_t most_groups = std::max<int64_t>(1, (1 << 21) / Hkv);        // a grid holds fewer than 2^32 threads
+    const int64_t code_words = (int64_t)Hkv * c->head_dim;                    // of a group
     SelectLaunch l;
+    bool many = false;                                                        // some row of the launch has more than one group
     ampd_status st = AMPD_OK;
     // pages that the last group of a row may choose by score (its other groups: no more), or 0 if it takes all it has
     auto scored = [&](const SelectRow& x) -> int64_t {
@@ -78,6 +80,8 @@ ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const a
     };
     auto flush = [&]() {
         int64_t tiles = 0;
+        l.codes = false;
+        for (int i = 0; i < l.n; ++i) l.codes |= l.keys > 0 && l.rows[i].L > g;
         for (int i = 0; i < l.n; ++i) tiles += (groups_of(l.rows[i].L, g) + 15) / 16 * ((scored(l.rows[i]) + 15) / 16) * Hkv;
         l.score_tiles = score_tiles(tiles);
         const int per = score_pages(Hkv, l.score_tiles);
@@ -88,30 +92,40 @@ ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const a
         if (l.n > 0 && st == AMPD_OK) st = f(l);
         l.n = l.groups = l.score_blocks = 0;
         l.keys = l.max_keys = 0;
+        many = false;
     };
     int64_t row_off = 0, out0 = 0;
     for (int r = 0; r < b->num_reqs && st == AMPD_OK; ++r) {
         const int64_t C = b->h_ctx_len[r], L = b->h_incr_len[r], groups = groups_of(L, g);
-        const int64_t per_group = Hkv * key_stride(C + L, P);
         for (int64_t at = 0; at < groups && st == AMPD_OK;) {
-            if (l.n == SELECT_MAX_REQS || l.groups == most_groups || (l.keys > 0 && l.keys + per_group > SELECT_KEYS)) {
+            SelectRow x;
+            x.C = (int32_t)(C + at * g);
+            x.L = (int32_t)(L - at * g);
+            // words that the launch holds with this row in it, and that each of the row's groups adds
+            const bool scores = scored(x) > 0, codes = (l.keys > 0 || scores) && (many || groups - at > 1);
+            const int64_t per_group = (scores ? Hkv * key_stride(C + L, P) : 0) + (codes ? code_words : 0);
+            const int64_t used = l.keys + (codes ? l.groups * code_words : 0);
+            if (l.n == SELECT_MAX_REQS || l.groups == most_groups || (l.n > 0 && used + per_group > SELECT_WORDS)) {
                 flush();
                 if (st != AMPD_OK) break;
+                continue;
             }
-            const int64_t take = std::min({groups - at, most_groups - l.groups, std::max<int64_t>(1, (SELECT_KEYS - l.keys) / per_group)});
-            SelectRow& x = l.rows[l.n++];
-            x.C = (int32_t)(C + at * g);
+            const int64_t room = per_group > 0 ? std::max<int64_t>(1, (SELECT_WORDS - used) / per_group) : groups;
+            const int64_t take = std::min({groups - at, most_groups - l.groups, room});
             x.L = (int32_t)std::min(L - at * g, take * g);
             x.row_off = (int32_t)(row_off + at * g);
             x.req = r;
             x.out0 = (int32_t)(out0 + at);
             x.item0 = l.groups;
+            x.tile0 = 0;
             x.key0 = (uint32_t)(l.keys / 64);
+            many |= take > 1;
             l.groups += (int)take;
             if (const int64_t end = scored(x)) {
                 l.max_keys = std::max(l.max_keys, end - s->first_pages);
                 l.keys += take * Hkv * key_stride((int64_t)x.C + x.L, P);
             }
+            l.rows[l.n++] = x;
             at += take;
         }
         row_off += L;
@@ -122,15 +136,13 @@ ampd_status select_launches(const ampd_kv_cache* c, const ampd_batch* b, const a
 }
 
 void select_plan(const ampd_kv_cache* c, const ampd_batch* b, const ampd_page_selection* s, SelectPlan* out) {
-    int64_t groups = 0;
+    out->bytes = 256;
     select_launches(c, b, s, [&](const SelectLaunch& l) {
-        out->keys_bytes = std::max(out->keys_bytes, l.keys * 4);
-        groups = std::max(groups, (int64_t)l.groups);
+        // (a group's codes at least, also where no launch makes any)
+        out->bytes = std::max(out->bytes, l.code_offset() + (l.codes ? l.groups : 1) * (int64_t)c->num_kv_heads * 4 * c->head_dim);
         if (out->launches++ == 0) out->only = l;
         return AMPD_OK;
     });
-    out->keys_bytes = (out->keys_bytes + 255) / 256 * 256;
-    out->bytes = std::max<int64_t>(256, out->keys_bytes + groups * c->num_kv_heads * 4 * c->head_dim);
 }
 
 void sparse_plan(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, int32_t g, SparsePlan* out) {
