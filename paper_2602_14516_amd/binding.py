@@ -569,8 +569,18 @@ def _output(name, shape, dtype, q, stream):
         return torch.empty(shape, dtype=getattr(torch, dtype), device=q.device)
 
 
+def _int32(name, x):
+    """A number that the library takes in 32 bits (ctypes would cut it)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name}: {x} does not fit 32 bits")
+    return x
+
+
 def num_groups(incr_len, group_tokens=1) -> int:
     """Groups of group_tokens consecutive new tokens that a batch has: rows of a selection."""
+    if _int32("group_tokens", group_tokens) < 1:
+        raise ValueError(f"group_tokens: at least 1 is wanted, not {group_tokens}")
     L = np.asarray(incr_len, dtype=np.int64)
     return int((-(-L // int(group_tokens))).sum())
 
@@ -634,7 +644,8 @@ def page_bounds_update(cache: KVCache, ctx_len, incr_len, block_table, bounds: P
 
 
 def _selection(budget, first_pages, last_pages, group_tokens):
-    return _Selection(int(budget), int(first_pages), int(last_pages), int(group_tokens), (ctypes.c_int32 * 4)())
+    return _Selection(_int32("budget", budget), _int32("first_pages", first_pages), _int32("last_pages", last_pages), _int32("group_tokens", group_tokens),
+                      (ctypes.c_int32 * 4)())
 
 
 def select_pages_workspace_bytes(cache: KVCache, ctx_len, incr_len, max_pages, budget, *, first_pages=1, last_pages=1, group_tokens=1) -> int:
@@ -659,11 +670,11 @@ def select_pages(cache: KVCache, ctx_len, incr_len, block_table, bounds: PageBou
     _want_table(block_table, len(ctx))
     _want_bounds(cache, bounds)
     _want("q", q, "bfloat16", (int(inc.sum()), cache.num_q_heads, cache.head_dim))
+    s = _selection(budget, first_pages, last_pages, group_tokens)
     shape = (num_groups(inc, group_tokens), cache.num_kv_heads, int(budget))
     if out is None:
         out = _output("out", shape, "int32", q, stream)
     _want("out", out, "int32", shape)
-    s = _selection(budget, first_pages, last_pages, group_tokens)
     b, keep = _batch_arg(ctx, inc, block_table, block_table_host)
     c = _selecting_cache(cache, bounds)
     if workspace is None:
@@ -687,7 +698,7 @@ def _selecting_cache(cache: KVCache, bounds: PageBounds):
 def sparse_attn_workspace_bytes(cache: KVCache, ctx_len, incr_len, max_pages, budget, *, group_tokens=1) -> int:
     b, keep = _batch(ctx_len, incr_len, None, max_pages=max_pages)
     c = cache.c_struct()
-    return int(lib.ampd_sparse_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(b), int(budget), int(group_tokens)))
+    return int(lib.ampd_sparse_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(b), _int32("budget", budget), _int32("group_tokens", group_tokens)))
 
 
 def sparse_attn(cache: KVCache, ctx_len, incr_len, block_table, selected, q, *, group_tokens=1, out=None, workspace=None, stream=None,
@@ -707,7 +718,7 @@ def sparse_attn(cache: KVCache, ctx_len, incr_len, block_table, selected, q, *, 
     _want("selected", selected, "int32")
     if selected.ndim != 3 or tuple(selected.shape[:2]) != (num_groups(inc, group_tokens), cache.num_kv_heads):
         raise ValueError(f"selected: [{num_groups(inc, group_tokens)}, {cache.num_kv_heads}, budget] is wanted, not {tuple(selected.shape)}")
-    budget = int(selected.shape[2])
+    budget = _int32("budget", selected.shape[2])
     if out is None:
         out = _output("out", shape, "bfloat16", q, stream)
     _want("out", out, "bfloat16", shape)
