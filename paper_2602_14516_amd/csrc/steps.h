@@ -205,10 +205,10 @@ __device__ __forceinline__ float exp_sum(float c, float m_use, bool rounded, Log
     return rounded ? rounded_sum : sum;
 }
 
-// O^T += V^T P^T for the 32 keys whose LDS tile starts at vl.
+// O^T += V^T P^T for the 32 keys whose LDS tile starts at vl; P: a row's probabilities, in one part or as the sum of several.
 // k-slot s of MFMA cc is key 16*cc + 8*(s/4) + 4*(lane/32) + s%4 of the block.
-template <int D>
-__device__ __forceinline__ void pv32(uint32_t vl, const bf16x8 (&P)[2], WaveAcc<D>& st, int lane) {
+template <int D, int PARTS>
+__device__ __forceinline__ void pv32_parts(uint32_t vl, const bf16x8 (&P)[PARTS][2], WaveAcc<D>& st, int lane) {
     using G_ = Geo<D>;
     const int g = lane >> 5, hi = (lane >> 4) & 1, i16 = lane & 15;
     // the 16 lanes of a transpose read address 4 keys (4*g + i16/4 ..) x 16 consecutive d
@@ -225,9 +225,15 @@ __device__ __forceinline__ void pv32(uint32_t vl, const bf16x8 (&P)[2], WaveAcc<
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, a0));
             const s16x4 hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, a0 + K8));
             const s16x8 av = {lo[0], lo[1], lo[2], lo[3], hi4[0], hi4[1], hi4[2], hi4[3]};
-            st.O[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), P[cc], st.O[db], 0, 0, 0);
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part)
+                st.O[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), P[part][cc], st.O[db], 0, 0, 0);
         }
     }
+}
+template <int D>
+__device__ __forceinline__ void pv32(uint32_t vl, const bf16x8 (&P)[2], WaveAcc<D>& st, int lane) {
+    pv32_parts<D, 1>(vl, reinterpret_cast<const bf16x8(&)[1][2]>(P), st, lane);
 }
 
 // One 32-key block, straight: used by narrow items (bandwidth-bound, no pipelining needed).
@@ -310,8 +316,8 @@ __device__ __forceinline__ void raise_reference16(WaveAcc16<D>& st, float mx) {
     st.m = m_new;
 }
 
-template <int D>
-__device__ __forceinline__ void pv16(uint32_t vl, const bf16x8& P, WaveAcc16<D>& st, int lane) {
+template <int D, int PARTS>
+__device__ __forceinline__ void pv16_parts(uint32_t vl, const bf16x8 (&P)[PARTS], WaveAcc16<D>& st, int lane) {
     using G_ = Geo<D>;
     const int g = lane >> 4, i16 = lane & 15;
     // the 16 lanes of a transpose read address 4 keys x 16 consecutive d and receive 4 keys of one d each
@@ -324,8 +330,14 @@ __device__ __forceinline__ void pv16(uint32_t vl, const bf16x8& P, WaveAcc16<D>&
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, a0));
         const s16x4 hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, a0 + K16));
         const s16x8 av = {lo[0], lo[1], lo[2], lo[3], hi4[0], hi4[1], hi4[2], hi4[3]};
-        st.O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), P, st.O[dt], 0, 0, 0);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part)
+            st.O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), P[part], st.O[dt], 0, 0, 0);
     }
+}
+template <int D>
+__device__ __forceinline__ void pv16(uint32_t vl, const bf16x8& P, WaveAcc16<D>& st, int lane) {
+    pv16_parts<D, 1>(vl, reinterpret_cast<const bf16x8(&)[1]>(P), st, lane);
 }
 
 // S^T and its softmax; P = the operand of the second product
