@@ -155,6 +155,32 @@ void sparse_plan(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, in
     out->bytes = std::max<int64_t>(256, floats * 4);
 }
 
+// Waves of a workgroup, and pieces of a list, for `items` lists (of a group, row tile and KV head) of so many keys.  A CU holds as many waves either
+// way: two workgroups of 4 waves or one of 8 at d = 128, by their LDS, twice as many at d = 64.  Cutting a list costs a second launch and the
+// partial results' way through memory, about 4 us.  us per call, of rows whose histories are four times as long as their lists:
+//                                            512 keys      2 048          8 192
+//    32 items, bf16, d = 128: 8 waves           9.2         24.7          85         4 waves, 16 pieces   9.9   13.2   30
+//    64                       8 waves          10.6         26.4          88         8 waves, 4 pieces   12.0   18.9   51      (4 waves, 8 pieces 18.7, 52)
+//   128                       8 waves          11.6         29.8         101         8 waves, 2 pieces   13.2   29.7   93
+//   128, 8 bits               8 waves           9.5         21.9          72         8 waves, 2 pieces   11.8   19.8   53
+//   192                       8 waves          12.7         37.0         129         4 waves, 4 pieces   17.7   40.7  134      (4 waves 13.0, 39.5, 146)
+//   264                       4 waves          19.7         62.5         238         4 waves, 3 pieces   23.4   57.0  192      (8 waves 23.1, 67.0, 239)
+//   384                       4 waves          22.5         71.1         284         4 waves, 3 pieces   26.1   76.7  264
+//   288, 32 rows              4 waves          13.8         33.3         112         4 waves, 3 pieces   24.6   40.2   98
+//   320, 8 bits, d = 64       4 waves           9.4         26.0          86         8 waves              9.1   21.1   69
+// Just above 256 items some CUs get two lists and most get one; thirds are spread more evenly.  What the rule does not take: 160 items over 8 192 keys are
+// up to a quarter faster in three pieces, 640 as much by 8 waves or in pieces.
+struct SparseCut {
+    int waves;
+    int64_t pieces;
+};
+static SparseCut sparse_cut(int64_t items, int64_t keys, int d, int tile) {
+    const bool long_lists = keys * d > 96 << 10;      // 768 keys at d = 128: whole 10 to 11 us, in pieces 9.5 to 12
+    if (items <= 32 && long_lists) return {4, std::min(512 / items, std::max<int64_t>(16, keys / 512))};     // (the join takes 16 pieces at once)
+    if (items <= 256) return {8, long_lists ? 256 / items : 1};
+    return {items <= 256 * 128 / d ? 8 : 4, items <= 341 && keys * d >= (int64_t)tile << 14 ? 3 : 1};
+}
+
 ampd_status sparse_launches(const ampd_kv_cache* c, const ampd_batch* b, int32_t budget, int32_t g, LaunchFn<SparseLaunch> f) {
     const int Hkv = c->num_kv_heads, rows = g * (c->num_q_heads / Hkv), tile = sparse_tile(rows), tiles = (rows + tile - 1) / tile;
     const int64_t most_groups = std::max<int64_t>(1, (1 << 22) / ((int64_t)Hkv * tiles));     // a grid holds fewer than 2^32 threads
@@ -164,13 +190,11 @@ ampd_status sparse_launches(const ampd_kv_cache* c, const ampd_batch* b, int32_t
     auto flush = [&](int64_t next) {
         if (l.n > 0 && st == AMPD_OK) {
             l.tiles = tiles;
-            // Two workgroups of 4 waves to a CU fill the chip.  Half as many items, down to one for every other CU, go as workgroups of 8 waves
-            // (200 lists of 2 048 keys, 8 bits, d = 64: 16.0 us instead of 16.6 in two pieces and 4.0 for the join); fewer are cut into pieces, of a
-            // block of 32 keys per wave at least.
             const int64_t items = (int64_t)l.groups * tiles * Hkv;
-            l.waves = items >= 128 && items <= 256 ? 8 : 4;
-            const int64_t want = l.waves == 8 ? 1 : std::max<int64_t>(1, 512 / items), least = l.waves * 32;
-            const int64_t per = ((keys + want - 1) / want + least - 1) / least * least;
+            const SparseCut cut = sparse_cut(items, keys, c->head_dim, tile);
+            const int64_t least = cut.waves * 32;
+            const int64_t per = ((keys + cut.pieces - 1) / cut.pieces + least - 1) / least * least;
+            l.waves = cut.waves;
             l.chunk = (int)per;
             l.splits = (int)((keys + per - 1) / per);
             l.partial_floats = l.splits > 1 ? items * l.splits * tile * (c->head_dim + 2) : 0;
