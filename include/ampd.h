@@ -51,7 +51,8 @@
  * Errors: every entry point validates its arguments on the host first.  On
  * AMPD_ERR_INVALID_ARG / UNSUPPORTED / WORKSPACE / PAGE_RANGE nothing has been enqueued.
  * AMPD_ERR_HIP reports a failed HIP call (launch, copy); work enqueued before it stays
- * enqueued.  Re-issuing a call with the same arguments is idempotent.
+ * enqueued.  Re-issuing a call with the same arguments is idempotent, but for ampd_rope_kv_append in
+ * place (q_out = q), which would rotate the queries again.
  */
 #ifndef AMPD_H
 #define AMPD_H
@@ -298,7 +299,8 @@ typedef struct {
  *       of the KV head's heads;
  *   n = sum over channels x of (sum of max(c, 0) over the group) * codes[0][x] + (sum of min(c, 0)) * codes[1][x];
  *   score = n rounded to 32-bit floating point, times the page's scale.
- * n is a whole number below 2^31, so the choice does not depend on any order of summation.
+ * n is a whole number below 2^31, so the choice does not depend on any order of summation: for given q, bounds and lengths there is
+ * one right list.  (Rotated queries are within a bound, not one byte image: another implementation's may choose otherwise at a near tie.)
  * q: DEVICE bf16 [sum L][Hq][d], 16-byte aligned, finite.  The cache's pools are not read.
  * workspace: DEVICE, 256-byte aligned, >= ampd_select_pages_workspace_bytes() (0: invalid arguments). */
 size_t ampd_select_pages_workspace_bytes(const ampd_kv_cache *cache, const ampd_batch *batch, const ampd_page_selection *sel);

@@ -1031,7 +1031,7 @@ __global__ __launch_bounds__(64 * NW) void choose_pages_kernel(const SelectParam
 // A block's position in the list decides its page; the list entries of the wave's next 8 blocks come with one load, their page ids with
 // another that is made a block later, so that neither is waited for.
 // ONCE: every page is read by one group (rows of one group each): loads that leave no lines behind (96 rows of 128 pages: 144 -> 130 us).  Lists of
-// neighbouring groups share pages, and their lines (64 groups of one row, 42 us, 48 so).
+// neighbouring groups share pages, and their lines (64 groups of one row: 42 us, 48 so, when their probabilities went in one part).
 template <int D, int KVT, bool ONCE>
 struct ListLoader {
     using G_ = Geo<D>;
@@ -1172,12 +1172,13 @@ constexpr int sparse_smem() {
 // An item: the rows of a group (tokens x heads of a KV head, ROWS at a time) over a piece of the group's list.  The waves take the piece's
 // blocks of 32 keys in turn, each with a softmax state and an LDS region of its own, and the states are merged at the end.
 // Logits, running maximum, sum and output are held in 32 bits; the matrix cores take the probabilities of the second product in 16 bits, so they
-// go in two parts, one after the other over the same V operand (one part, rounded to bf16: 38 us instead of 41 for 64 groups of 32 rows, 129.7 instead of
-// 130.5 for 96 rows, and outputs 0.0021 off their 64-bit values, relative, instead of 0.0017, which is the rounding of the output alone).
+// go in two parts, one after the other over the same V operand (one part, rounded to bf16: 38 us instead of 41 for 64 groups of 32 rows, 129.4 instead of
+// 130.0 for 96 rows, and outputs 0.0021 off their 64-bit values, relative, instead of 0.0017, which is the rounding of the output alone).
 // Bound: memory where every list is another's (96 rows x 8 heads over 128 pages of 16, 809 MB in 130 us = 6.2 TB/s); LDS, through which K and V
-// pass on their way into the operands' layout, where 32 rows share a list that is in L2 (64 groups: 40 us, on pages that never leave L2 38, without its
-// products 31, without its loads 33, without what it writes to LDS 35: the three overlap but for a fifth, with two waves a SIMD; K loaded straight in
-// the layout of a 32x32x16 or two 16x16x32 products, quarter or half lines at a time, 52 and 50).
+// pass on their way into the operands' layout, and the products, where 32 rows share a list that is in L2 (64 groups by the trace: 45 us, on pages that
+// never leave L2 42, without its products 32, without its loads 38, without what it writes to LDS 38; two waves a SIMD.  K loaded straight in
+// the layout of a 32x32x16 or two 16x16x32 products, quarter or half lines at a time, took 52 and 50 where this took 42).  A group of more rows
+// goes as tiles of 32 that stage its list again each (64 groups of 64 rows 80 us, 32 of 128 rows 78).
 template <int D, int KVT, int ROWS, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 2) void sparse_rows_kernel(const SparseParams p) {
     using G_ = Geo<D>;
